@@ -419,6 +419,142 @@ ifvs_status ifvs_train_step(ifvs_index* idx, int32_t nq, const float* q, const i
  * Errors: IFVS_E_STATE (no memory bank), IFVS_E_HIP. */
 ifvs_status ifvs_read_params(const ifvs_index* idx, float* bank_out, float* W_out, void* stream);
 
+/* ---- Row operators -------------------------------------------------------
+ * What training and evaluating the conditioning need beside ifvs_train_step:
+ * a lookup in any table of rows and its gradient (the memory bank of Section
+ * 2's opening paragraph is one such table; a table of predicate weights, whose
+ * gradient ifvs_train_step returns as dL/dw_z, another), the log
+ * probabilities that rows of scores give to their columns, and a loss that
+ * follows a teacher's scores.  They take no index handle: they run on the
+ * current device, allocate nothing, keep nothing between calls and may be
+ * captured into a HIP graph.  Scratch is the caller's: `workspace` is
+ * device memory of at least the bytes the matching *_workspace call gives,
+ * 16-byte aligned, with any contents; calls that may overlap (other streams,
+ * graphs replayed side by side) need a workspace each.  Rows are counted from
+ * their first element at strides (`*_ld`, in elements) of at least the row's
+ * length; columns are contiguous; no alignment beyond the element's is needed.
+ * Sums are fp32 or fp64 in a fixed order: equal calls give equal bits. */
+#define IFVS_ELEM_F32  0
+#define IFVS_ELEM_F16  1
+#define IFVS_ELEM_BF16 2
+#define IFVS_MAX_BAG   16
+#define IFVS_MAX_TOP   32
+#define IFVS_MAX_COLS  (1 << 21)
+
+/* ifvs_embed_lookup -- out[i] = scale * sum over j < bag of table[ids[i][j]],
+ * the sum in j order from +0 in fp32, one rounding to the element type at the
+ * end.  An id outside 0..rows-1 (such as -1) is an absent slot; a row with no
+ * present slot is 0.
+ *  table: device [rows] rows of dim elements of type dtype, table_ld apart
+ *  ids:   device [n][bag] int32
+ *  out:   device [n] rows of dim elements of type dtype, out_ld apart; must
+ *         not overlap the table
+ * Enqueued on `stream`; n = 0 writes nothing.
+ * Errors: IFVS_E_INVALID (rows outside 1..2^31-2, dim outside 1..2^20, bag
+ * outside 1..IFVS_MAX_BAG, n * bag outside 0..2^30, a stride below dim,
+ * non-finite scale, unknown dtype, NULL or misaligned arrays), IFVS_E_HIP. */
+ifvs_status ifvs_embed_lookup(int64_t rows, int32_t dim, const void* table, int64_t table_ld, int32_t dtype,
+                              int64_t n, int32_t bag, const int32_t* ids, float scale, void* out, int64_t out_ld,
+                              void* stream);
+
+/* Bytes of ifvs_embed_gradient's workspace; -1 when a size is out of range. */
+int64_t ifvs_embed_workspace(int64_t rows, int32_t dim, int64_t n, int32_t bag);
+
+/* ifvs_embed_gradient -- the gradient of ifvs_embed_lookup's table: with the
+ * present slots sorted by table row (equal rows in slot order),
+ *   G[r] = scale * sum over slots (i, j) with ids[i][j] = r of grad[i],
+ * summed in fp32 in an order fixed by the ids alone, rounded once.
+ *  grad:       device [n] rows of dim elements of type dtype, grad_ld apart
+ *  accumulate: 0: table_grad = G, rows that no slot names become 0;
+ *              1: table_grad += G, only rows that a slot names are touched
+ *  table_grad: device [rows] rows of dim elements of type out_dtype
+ *              (IFVS_ELEM_F32 or dtype), out_ld apart; must not overlap grad
+ * Enqueued on `stream`.  n = 0 with accumulate = 0 clears table_grad.
+ * Errors: as ifvs_embed_lookup, plus IFVS_E_INVALID for accumulate not 0 or
+ * 1, another out_dtype, a missing, small or misaligned workspace. */
+ifvs_status ifvs_embed_gradient(int64_t rows, int32_t dim, int64_t n, int32_t bag, const int32_t* ids, float scale,
+                                const void* grad, int64_t grad_ld, int32_t dtype, int32_t accumulate,
+                                void* table_grad, int64_t out_ld, int32_t out_dtype, void* workspace,
+                                int64_t workspace_bytes, void* stream);
+
+/* Bytes of ifvs_log_probs' workspace; -1 when a size is out of range. */
+int64_t ifvs_log_probs_workspace(int64_t n, int64_t cols, int32_t n_top);
+
+/* ifvs_log_probs -- each row's distribution q = softmax(logits / tau) over its
+ * columns v < n_valid[i] (others are not read, whatever they hold):
+ *   given_out[i][g] = log q[given[i][g]]; -inf for a column outside
+ *                     0..n_valid[i]-1 (an absent slot, such as -1)
+ *   entropy_out[i]  = -sum over v of q_v log q_v
+ *   top_ids_out[i], top_out[i]: the n_top columns of the largest logits in
+ *     descending order, ties to the lower column, and their log q; columns of
+ *     logit -inf are no alternatives, missing ones are (-1, -inf)
+ * A logit of -inf has probability 0.  A row without a column above -inf has
+ * no distribution: -inf, entropy 0, no alternatives.  A row with a NaN or a
+ * +inf logit: NaN for its present given columns and its entropy, no
+ * alternatives (-1, NaN).
+ *  logits:  device [n] rows of cols elements of type dtype, ld apart
+ *  n_valid: device [n] int32 (values outside 0..cols are clamped), or NULL:
+ *           every column
+ *  given:   device [n][n_given] int32, NULL when n_given = 0
+ *  given_out [n][n_given], entropy_out [n], top_ids_out [n][n_top] int32,
+ *  top_out [n][n_top]: device, fp32; entropy_out may be NULL, the others when
+ *           their count is 0
+ * Enqueued on `stream`; n = 0 writes nothing.
+ * Errors: IFVS_E_INVALID (n outside 0..2^31-1, cols outside
+ * 1..IFVS_MAX_COLS, n_given outside 0..IFVS_MAX_K, n_top outside
+ * 0..IFVS_MAX_TOP, ld < cols, tau not positive and finite or 1 / tau not
+ * finite, unknown dtype, NULL or misaligned arrays, a missing, small or
+ * misaligned workspace), IFVS_E_HIP. */
+ifvs_status ifvs_log_probs(int64_t n, int64_t cols, const void* logits, int64_t ld, int32_t dtype,
+                           const int32_t* n_valid, float tau, const int32_t* given, int32_t n_given, int32_t n_top,
+                           float* given_out, float* entropy_out, int32_t* top_ids_out, float* top_out,
+                           void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of ifvs_distill_loss' workspace; -1 when a size is out of range. */
+int64_t ifvs_distill_workspace(int64_t n, int64_t cols);
+
+/* ifvs_distill_loss -- the distillation loss of each row of student logits
+ * from a teacher known by its n_teacher largest logits, and its gradient.
+ * q = softmax(logits / tau) over the columns v < n_valid[i]; teacher slot k
+ * names column teacher_ids[i][k], absent when outside 0..n_valid[i]-1 (such
+ * as -1).  With teacher_lse NULL the teacher's distribution is
+ * p = softmax(teacher_logits / tau) over the present slots:
+ *   loss_out[i] = tau^2 sum_k p_k (log p_k - log q_k)
+ *   dL/dz_v     = tau (q_v - p_v)
+ * With teacher_lse (the logarithm of the sum of exp(t / tau) over all of the
+ * teacher's logits) p_k = exp(t_k / tau - lse), and what is left,
+ * P = max(0, 1 - sum p_k), belongs to the columns that no slot names, as one
+ * class of student probability Q = sum of their q_v:
+ *   loss_out[i] = tau^2 [ sum_k p_k (log p_k - log q_k) + P (log P - log Q) ]
+ *   dL/dz_v     = tau (q_v - p_v) of a named column,
+ *                 tau (q_v - P q_v / Q) of another one
+ * (P = 0 where no other column has a logit above -inf.)  Terms of probability
+ * 0 are 0; a column that several slots name has the sum of their p.
+ * grad_out = row_weight[i] * dL/dz, rounded once, and 0 in the columns from
+ * n_valid[i] on.  A row of weight 0 is left out: loss 0, gradient 0, nothing
+ * of it read.  So is a row that has no present slot and no teacher_lse, or no
+ * column above -inf.  A NaN or +inf among a row's logits or its present
+ * teacher logits makes its loss and gradient NaN, and so do, without
+ * teacher_lse, present teacher logits that are all -inf.
+ *  logits: device [n] rows of cols elements of type dtype, ld apart
+ *  n_valid: device [n] int32 (clamped to 0..cols), or NULL
+ *  teacher_ids: device [n][n_teacher] int32; teacher_logits: device
+ *           [n][n_teacher] fp32; teacher_lse: device [n] fp32 or NULL
+ *  row_weight: device [n] fp32, or NULL: 1
+ *  loss_out: device [n] fp32 (not weighted)
+ *  grad_out: device [n] rows of cols elements of type dtype, grad_ld apart,
+ *           or NULL: the loss alone.  May be the logits themselves (the same
+ *           pointer and stride), else it must not overlap them.
+ * Enqueued on `stream`; n = 0 writes nothing.
+ * Errors: IFVS_E_INVALID (n, cols, dtype, tau, strides and workspace as in
+ * ifvs_log_probs, n_teacher outside 1..IFVS_MAX_K, NULL or misaligned arrays),
+ * IFVS_E_HIP. */
+ifvs_status ifvs_distill_loss(int64_t n, int64_t cols, const void* logits, int64_t ld, int32_t dtype,
+                              const int32_t* n_valid, int32_t n_teacher, const int32_t* teacher_ids,
+                              const float* teacher_logits, const float* teacher_lse, float tau,
+                              const float* row_weight, float* loss_out, void* grad_out, int64_t grad_ld,
+                              void* workspace, int64_t workspace_bytes, void* stream);
+
 /* ifvs_load_reconstructions -- attach, in place of full-precision vectors,
  * the reconstructions of the index's own codes: row i becomes the
  * concatenation over m of codeword C_PQ[m][code_i[m]].  ifvs_exact_search

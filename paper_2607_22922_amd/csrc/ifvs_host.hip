@@ -2557,6 +2557,209 @@ ifvs_status ifvs_train_step(ifvs_index* idx, int32_t nq, const float* q, const i
   return IFVS_OK;
 }
 
+// ---- row operators
+namespace {
+
+size_t elem_bytes(int32_t dtype) { return dtype == IFVS_ELEM_F32 ? 4 : 2; }
+
+bool known_elem(int32_t dtype) {
+  return dtype == IFVS_ELEM_F32 || dtype == IFVS_ELEM_F16 || dtype == IFVS_ELEM_BF16;
+}
+
+bool aligned_to(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+bool embed_sizes_ok(int64_t rows, int32_t dim, int64_t n, int32_t bag) {
+  return rows >= 1 && rows <= (int64_t(1) << 31) - 2 && dim >= 1 && dim <= (1 << 20) && bag >= 1 &&
+         bag <= IFVS_MAX_BAG && n >= 0 && n <= (int64_t(1) << 30) / bag;
+}
+
+bool row_sizes_ok(int64_t n, int64_t cols) {
+  return n >= 0 && n < (int64_t(1) << 31) && cols >= 1 && cols <= IFVS_MAX_COLS;
+}
+
+ifvs_status check_workspace(const void* workspace, int64_t have, int64_t need) {
+  if (need == 0) return IFVS_OK;
+  if (!workspace || have < need)
+    return fail(IFVS_E_INVALID, "the workspace has " + std::to_string(workspace ? have : 0) + " bytes, the call needs " +
+                                    std::to_string(need));
+  if (!aligned_to(workspace, 16)) return fail(IFVS_E_INVALID, "the workspace is not 16-byte aligned");
+  return IFVS_OK;
+}
+
+ifvs_status check_embed(int64_t rows, int32_t dim, int64_t n, int32_t bag, const int32_t* ids, float scale,
+                        int32_t dtype) {
+  if (!embed_sizes_ok(rows, dim, n, bag))
+    return fail(IFVS_E_INVALID, "rows, dim, bag or n * bag out of range (rows 1..2^31-2, dim 1..2^20, bag 1..16, "
+                                "n * bag 0..2^30)");
+  if (!known_elem(dtype)) return fail(IFVS_E_INVALID, "unknown element type");
+  if (!std::isfinite(scale)) return fail(IFVS_E_INVALID, "scale must be finite");
+  if (n > 0 && (!ids || !aligned_to(ids, 4))) return fail(IFVS_E_INVALID, "ids is NULL or misaligned");
+  return IFVS_OK;
+}
+
+// The checks that ifvs_log_probs and ifvs_distill_loss share.
+ifvs_status check_rows(int64_t n, int64_t cols, const void* logits, int64_t ld, int32_t dtype, const int32_t* n_valid,
+                       float tau) {
+  if (!row_sizes_ok(n, cols)) return fail(IFVS_E_INVALID, "n or cols out of range (n 0..2^31-1, cols 1..2^21)");
+  if (!known_elem(dtype)) return fail(IFVS_E_INVALID, "unknown element type");
+  if (ld < cols) return fail(IFVS_E_INVALID, "the row stride of the logits is below cols");
+  if (!(tau > 0.0f) || !std::isfinite(tau) || !std::isfinite(1.4426950408889634f / tau))
+    return fail(IFVS_E_INVALID, "tau must be positive and finite, and so must 1 / tau");
+  if (n > 0 && (!logits || !aligned_to(logits, elem_bytes(dtype))))
+    return fail(IFVS_E_INVALID, "logits is NULL or misaligned");
+  if (!aligned_to(n_valid, 4)) return fail(IFVS_E_INVALID, "n_valid is misaligned");
+  return IFVS_OK;
+}
+
+}  // namespace
+
+ifvs_status ifvs_embed_lookup(int64_t rows, int32_t dim, const void* table, int64_t table_ld, int32_t dtype,
+                              int64_t n, int32_t bag, const int32_t* ids, float scale, void* out, int64_t out_ld,
+                              void* stream) {
+  if (ifvs_status st = check_embed(rows, dim, n, bag, ids, scale, dtype); st != IFVS_OK) return st;
+  if (table_ld < dim || out_ld < dim) return fail(IFVS_E_INVALID, "a row stride is below dim");
+  if (n == 0) return IFVS_OK;
+  if (!table || !aligned_to(table, elem_bytes(dtype)) || !out || !aligned_to(out, elem_bytes(dtype)))
+    return fail(IFVS_E_INVALID, "table or out is NULL or misaligned");
+  EmbedArgs a{};
+  a.rows = rows;
+  a.dim = dim;
+  a.n = n;
+  a.bag = bag;
+  a.ids = ids;
+  a.scale = scale;
+  a.dtype = dtype;
+  a.table = table;
+  a.table_ld = table_ld;
+  a.out = out;
+  a.out_ld = out_ld;
+  IFVS_HIP(launch_embed_lookup(a, static_cast<hipStream_t>(stream)), "launching embedding lookup");
+  return IFVS_OK;
+}
+
+int64_t ifvs_embed_workspace(int64_t rows, int32_t dim, int64_t n, int32_t bag) {
+  return embed_sizes_ok(rows, dim, n, bag) ? embed_workspace_bytes(rows, dim, n * bag) : -1;
+}
+
+ifvs_status ifvs_embed_gradient(int64_t rows, int32_t dim, int64_t n, int32_t bag, const int32_t* ids, float scale,
+                                const void* grad, int64_t grad_ld, int32_t dtype, int32_t accumulate,
+                                void* table_grad, int64_t out_ld, int32_t out_dtype, void* workspace,
+                                int64_t workspace_bytes, void* stream) {
+  if (ifvs_status st = check_embed(rows, dim, n, bag, ids, scale, dtype); st != IFVS_OK) return st;
+  if (out_dtype != IFVS_ELEM_F32 && out_dtype != dtype)
+    return fail(IFVS_E_INVALID, "out_dtype must be IFVS_ELEM_F32 or dtype");
+  if (accumulate != 0 && accumulate != 1) return fail(IFVS_E_INVALID, "accumulate must be 0 or 1");
+  if (grad_ld < dim || out_ld < dim) return fail(IFVS_E_INVALID, "a row stride is below dim");
+  if (n == 0 && accumulate) return IFVS_OK;
+  if ((n > 0 && (!grad || !aligned_to(grad, elem_bytes(dtype)))) || !table_grad ||
+      !aligned_to(table_grad, elem_bytes(out_dtype)))
+    return fail(IFVS_E_INVALID, "grad or table_grad is NULL or misaligned");
+  if (ifvs_status st = check_workspace(workspace, workspace_bytes, embed_workspace_bytes(rows, dim, n * bag));
+      st != IFVS_OK)
+    return st;
+  EmbedArgs a{};
+  a.rows = rows;
+  a.dim = dim;
+  a.n = n;
+  a.bag = bag;
+  a.ids = ids;
+  a.scale = scale;
+  a.dtype = dtype;
+  a.grad = grad;
+  a.grad_ld = grad_ld;
+  a.out_dtype = out_dtype;
+  a.accumulate = accumulate;
+  a.out = table_grad;
+  a.out_ld = out_ld;
+  a.workspace = workspace;
+  IFVS_HIP(launch_embed_gradient(a, static_cast<hipStream_t>(stream)), "launching embedding gradient");
+  return IFVS_OK;
+}
+
+int64_t ifvs_log_probs_workspace(int64_t n, int64_t cols, int32_t n_top) {
+  return row_sizes_ok(n, cols) && n_top >= 0 && n_top <= IFVS_MAX_TOP ? log_probs_workspace_bytes(n, cols, n_top) : -1;
+}
+
+ifvs_status ifvs_log_probs(int64_t n, int64_t cols, const void* logits, int64_t ld, int32_t dtype,
+                           const int32_t* n_valid, float tau, const int32_t* given, int32_t n_given, int32_t n_top,
+                           float* given_out, float* entropy_out, int32_t* top_ids_out, float* top_out,
+                           void* workspace, int64_t workspace_bytes, void* stream) {
+  if (ifvs_status st = check_rows(n, cols, logits, ld, dtype, n_valid, tau); st != IFVS_OK) return st;
+  if (n_given < 0 || n_given > IFVS_MAX_K) return fail(IFVS_E_INVALID, "n_given must be in 0..1024");
+  if (n_top < 0 || n_top > IFVS_MAX_TOP) return fail(IFVS_E_INVALID, "n_top must be in 0..32");
+  if (n == 0) return IFVS_OK;
+  if (n_given > 0 && (!given || !given_out || !aligned_to(given, 4) || !aligned_to(given_out, 4)))
+    return fail(IFVS_E_INVALID, "given or given_out is NULL or misaligned");
+  if (n_top > 0 && (!top_ids_out || !top_out || !aligned_to(top_ids_out, 4) || !aligned_to(top_out, 4)))
+    return fail(IFVS_E_INVALID, "top_ids_out or top_out is NULL or misaligned");
+  if (!aligned_to(entropy_out, 4)) return fail(IFVS_E_INVALID, "entropy_out is misaligned");
+  if (ifvs_status st = check_workspace(workspace, workspace_bytes, log_probs_workspace_bytes(n, cols, n_top));
+      st != IFVS_OK)
+    return st;
+  LogProbArgs a{};
+  a.n = n;
+  a.cols = cols;
+  a.logits = logits;
+  a.ld = ld;
+  a.dtype = dtype;
+  a.n_valid = n_valid;
+  a.c = 1.4426950408889634f / tau;
+  a.given = given;
+  a.n_given = n_given;
+  a.n_top = n_top;
+  a.given_out = given_out;
+  a.entropy_out = entropy_out;
+  a.top_ids_out = top_ids_out;
+  a.top_out = top_out;
+  a.workspace = workspace;
+  IFVS_HIP(launch_log_probs(a, static_cast<hipStream_t>(stream)), "launching log probabilities");
+  return IFVS_OK;
+}
+
+int64_t ifvs_distill_workspace(int64_t n, int64_t cols) {
+  return row_sizes_ok(n, cols) ? distill_workspace_bytes(n, cols) : -1;
+}
+
+ifvs_status ifvs_distill_loss(int64_t n, int64_t cols, const void* logits, int64_t ld, int32_t dtype,
+                              const int32_t* n_valid, int32_t n_teacher, const int32_t* teacher_ids,
+                              const float* teacher_logits, const float* teacher_lse, float tau,
+                              const float* row_weight, float* loss_out, void* grad_out, int64_t grad_ld,
+                              void* workspace, int64_t workspace_bytes, void* stream) {
+  if (ifvs_status st = check_rows(n, cols, logits, ld, dtype, n_valid, tau); st != IFVS_OK) return st;
+  if (n_teacher < 1 || n_teacher > IFVS_MAX_K) return fail(IFVS_E_INVALID, "n_teacher must be in 1..1024");
+  if (grad_out && grad_ld < cols) return fail(IFVS_E_INVALID, "the row stride of the gradient is below cols");
+  if (n == 0) return IFVS_OK;
+  if (!teacher_ids || !teacher_logits || !loss_out || !aligned_to(teacher_ids, 4) || !aligned_to(teacher_logits, 4) ||
+      !aligned_to(loss_out, 4))
+    return fail(IFVS_E_INVALID, "teacher_ids, teacher_logits or loss_out is NULL or misaligned");
+  if (!aligned_to(teacher_lse, 4) || !aligned_to(row_weight, 4) || !aligned_to(grad_out, elem_bytes(dtype)))
+    return fail(IFVS_E_INVALID, "teacher_lse, row_weight or grad_out is misaligned");
+  if (grad_out == logits && grad_ld != ld)
+    return fail(IFVS_E_INVALID, "a gradient in the logits' place needs their row stride");
+  if (ifvs_status st = check_workspace(workspace, workspace_bytes, distill_workspace_bytes(n, cols)); st != IFVS_OK)
+    return st;
+  DistillArgs a{};
+  a.n = n;
+  a.cols = cols;
+  a.logits = logits;
+  a.ld = ld;
+  a.dtype = dtype;
+  a.n_valid = n_valid;
+  a.n_teacher = n_teacher;
+  a.teacher_ids = teacher_ids;
+  a.teacher_logits = teacher_logits;
+  a.teacher_lse = teacher_lse;
+  a.tau = tau;
+  a.c = 1.4426950408889634f / tau;
+  a.row_weight = row_weight;
+  a.loss_out = loss_out;
+  a.grad_out = grad_out;
+  a.grad_ld = grad_ld;
+  a.workspace = workspace;
+  IFVS_HIP(launch_distill(a, static_cast<hipStream_t>(stream)), "launching distillation loss");
+  return IFVS_OK;
+}
+
 ifvs_status ifvs_read_params(const ifvs_index* idx, float* bank_out, float* W_out, void* stream) {
   if (ifvs_status st = check_index(idx); st != IFVS_OK) return st;
   if (idx->bank_rows == 0) return fail(IFVS_E_STATE, "the index has no memory bank and W");

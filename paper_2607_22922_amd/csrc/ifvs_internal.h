@@ -555,4 +555,69 @@ struct ExactRerank {
 };
 hipError_t launch_exact_rerank(const ExactRerank& e, hipStream_t s);
 
+// Row operators (element types as IFVS_ELEM_* in ifvs.h).
+constexpr int kElemF32 = 0;
+constexpr int kElemF16 = 1;
+constexpr int kElemBF16 = 2;
+
+struct EmbedArgs {
+  int64_t rows;
+  int dim;
+  int64_t n;
+  int bag;
+  const int32_t* ids;        // [n][bag], absent outside 0..rows-1
+  float scale;
+  int dtype;                 // of table / out (lookup), of grad (gradient)
+  const void* table;         // lookup: [rows] rows, table_ld apart
+  int64_t table_ld;
+  const void* grad;          // gradient: [n] rows, grad_ld apart
+  int64_t grad_ld;
+  int out_dtype;             // gradient: of out
+  int accumulate;            // gradient: add to out, hit rows only
+  void* out;                 // [n] (lookup) or [rows] (gradient) rows, out_ld apart
+  int64_t out_ld;
+  void* workspace;
+};
+int64_t embed_workspace_bytes(int64_t rows, int dim, int64_t slots);
+hipError_t launch_embed_lookup(const EmbedArgs& a, hipStream_t s);
+hipError_t launch_embed_gradient(const EmbedArgs& a, hipStream_t s);
+
+struct LogProbArgs {
+  int64_t n, cols;
+  const void* logits;
+  int64_t ld;
+  int dtype;
+  const int32_t* n_valid;    // [n] or null
+  float c;                   // log2(e) / tau
+  const int32_t* given;      // [n][n_given]
+  int n_given, n_top;
+  float* given_out;
+  float* entropy_out;        // or null
+  int32_t* top_ids_out;
+  float* top_out;
+  void* workspace;
+};
+int64_t log_probs_workspace_bytes(int64_t n, int64_t cols, int n_top);
+hipError_t launch_log_probs(const LogProbArgs& a, hipStream_t s);
+
+struct DistillArgs {
+  int64_t n, cols;
+  const void* logits;
+  int64_t ld;
+  int dtype;
+  const int32_t* n_valid;        // [n] or null
+  int n_teacher;
+  const int32_t* teacher_ids;    // [n][n_teacher], absent outside the row
+  const float* teacher_logits;   // [n][n_teacher]
+  const float* teacher_lse;      // [n] or null: p is a softmax over the slots
+  float tau, c;                  // c = log2(e) / tau
+  const float* row_weight;       // [n] or null (1)
+  float* loss_out;               // [n]
+  void* grad_out;                // [n] rows of cols, grad_ld apart; null: none; may be logits
+  int64_t grad_ld;
+  void* workspace;
+};
+int64_t distill_workspace_bytes(int64_t n, int64_t cols);
+hipError_t launch_distill(const DistillArgs& a, hipStream_t s);
+
 }  // namespace ifvs

@@ -31,6 +31,8 @@ OPT_SEED_TILES = 11
 OPT_COUNT_READS = 12
 OPT_COARSE = 13
 OPT_SCREEN = 14
+ELEM = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}     # IFVS_ELEM_*
+MAX_BAG, MAX_TOP, MAX_COLS = 16, 32, 1 << 21
 STAGES = ("condition", "lut", "filter", "scan", "merge", "encode", "coarse")
 
 EXPORTED = ("ifvs_load_index", "ifvs_free_index", "ifvs_select_codebook", "ifvs_build_lut",
@@ -40,7 +42,9 @@ EXPORTED = ("ifvs_load_index", "ifvs_free_index", "ifvs_select_codebook", "ifvs_
             "ifvs_filtered_search_noalloc", "ifvs_read_scan_reads", "ifvs_probe_lds_gather",
             "ifvs_encoder_params", "ifvs_load_encoder", "ifvs_encode_predicates",
             "ifvs_build_coarse", "ifvs_lut_bounds", "ifvs_filtered_search_bounded", "ifvs_read_coarse",
-            "ifvs_last_coarse", "ifvs_last_modes", "ifvs_query_batch")
+            "ifvs_last_coarse", "ifvs_last_modes", "ifvs_query_batch",
+            "ifvs_embed_lookup", "ifvs_embed_workspace", "ifvs_embed_gradient",
+            "ifvs_log_probs_workspace", "ifvs_log_probs", "ifvs_distill_workspace", "ifvs_distill_loss")
 
 
 class IfvsError(RuntimeError):
@@ -103,7 +107,7 @@ def _load_library() -> ctypes.CDLL:
         raise ImportError(f"{_LIB_PATH} is missing: build it with "
                           "`python -m paper_2607_22922_amd.build` (there is no fallback path)")
     lib = ctypes.CDLL(_LIB_PATH)
-    vp, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+    vp, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
     sig = {
         "ifvs_load_index": ([ctypes.POINTER(IndexDesc), ctypes.POINTER(vp)], i32),
         "ifvs_free_index": ([vp], None),
@@ -135,6 +139,14 @@ def _load_library() -> ctypes.CDLL:
         "ifvs_read_coarse": ([vp, ctypes.POINTER(i32), vp, vp, vp], i32),
         "ifvs_last_coarse": ([vp, ctypes.POINTER(i32)], i32),
         "ifvs_last_modes": ([vp, i32, vp], i32),
+        "ifvs_embed_lookup": ([i64, i32, vp, i64, i32, i64, i32, vp, f32, vp, i64, vp], i32),
+        "ifvs_embed_workspace": ([i64, i32, i64, i32], i64),
+        "ifvs_embed_gradient": ([i64, i32, i64, i32, vp, f32, vp, i64, i32, i32, vp, i64, i32, vp, i64, vp], i32),
+        "ifvs_log_probs_workspace": ([i64, i64, i32], i64),
+        "ifvs_log_probs": ([i64, i64, vp, i64, i32, vp, f32, vp, i32, i32, vp, vp, vp, vp, vp, i64, vp], i32),
+        "ifvs_distill_workspace": ([i64, i64], i64),
+        "ifvs_distill_loss": ([i64, i64, vp, i64, i32, vp, i32, vp, vp, vp, f32, vp, vp, vp, i64, vp, i64, vp],
+                              i32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -515,6 +527,179 @@ class Index:
         alpha, wf = self.select_codebook(q, preds, w_z)
         lut = self.build_lut(q, alpha if conditioned else None, wf, lut_dtype)
         return self.search(preds, lut, k, lut_dtype)
+
+
+# ------------------------------------------------------------ row operators
+def _rows_arg(t, name):
+    """A 2-D CUDA tensor of a known element type with contiguous columns and
+    rows that do not overlap; other layouts are copied."""
+    if t.dim() != 2 or not t.is_cuda or t.dtype not in ELEM:
+        raise IfvsError(E_INVALID, f"{name} must be a 2-D CUDA tensor of float32, float16 or bfloat16")
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1] or t.shape[1] > 1 and t.stride(1) != 1:
+        t = t.contiguous()
+    return t
+
+
+def _ld(t):
+    """Row stride of a tensor of _rows_arg (of one row any stride serves)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _small_arg(t, name, dtype, shape, device):
+    """A contiguous tensor of `dtype` and `shape` on `device` (None stays None)."""
+    if t is None:
+        return None
+    if tuple(t.shape) != shape or t.device != device:
+        raise IfvsError(E_INVALID, f"{name} must have shape {shape} and lie on {device}")
+    if t.dtype != dtype:
+        if dtype == torch.int32:
+            if t.is_floating_point() or t.is_complex() or t.dtype == torch.bool:
+                raise IfvsError(E_INVALID, f"{name} must be whole numbers")
+            t = t.clamp(-1, 0x7FFFFFFF)          # numbers past 32 bits must not wrap into range
+        t = t.to(dtype)
+    return t if t.is_contiguous() else t.contiguous()
+
+
+def _out_arg(t, name, dtype, shape, device):
+    """A caller's output: written in place, so it must fit as it is."""
+    ok = (tuple(t.shape) == shape and t.dtype == dtype and t.device == device and
+          (shape[1] <= 1 or t.stride(1) == 1) and (shape[0] <= 1 or t.stride(0) >= shape[1]))
+    if not ok:
+        raise IfvsError(E_INVALID, f"{name} must be {dtype}, {shape}, with contiguous columns, on {device}")
+    return t
+
+
+class _OnDevice:
+    """Makes a tensor's device the current one for a call (a no-op where it is
+    already), so its stream, allocations and launches belong together."""
+
+    def __init__(self, device):
+        self.device, self.before = device, None
+
+    def __enter__(self):
+        if self.device.index != torch.cuda.current_device():
+            self.before = torch.cuda.current_device()
+            torch.cuda.set_device(self.device)
+
+    def __exit__(self, *exc):
+        if self.before is not None:
+            torch.cuda.set_device(self.before)
+
+
+def _scratch(nbytes, device):
+    if nbytes < 0:
+        raise IfvsError(E_INVALID, "a size is out of range")
+    return torch.empty(nbytes, device=device, dtype=torch.uint8) if nbytes else None
+
+
+def _ids_arg(ids, device):
+    if ids.dim() == 1:
+        ids = ids[:, None]
+    if ids.dim() != 2:
+        raise IfvsError(E_INVALID, "ids must be [n] or [n][bag]")
+    return _small_arg(ids, "ids", torch.int32, tuple(ids.shape), device)
+
+
+def embed_lookup(table, ids, scale=1.0, out=None):
+    """ifvs_embed_lookup: out[i] = scale * sum over j of table[ids[i][j]].
+
+    table [rows][dim] (any row stride), ids [n] or [n][bag] (ids outside the
+    table are absent); returns [n][dim] in the table's type (`out` if given).
+    Enqueued on the current stream of the table's device."""
+    table = _rows_arg(table, "table")
+    dev = table.device
+    with _OnDevice(dev):
+        ids = _ids_arg(ids, dev)
+        n, dim = ids.shape[0], table.shape[1]
+        if out is None:
+            out = torch.empty(n, dim, device=dev, dtype=table.dtype)
+        else:
+            _out_arg(out, "out", table.dtype, (n, dim), dev)
+        _check(_lib.ifvs_embed_lookup(table.shape[0], dim, table.data_ptr(), _ld(table), ELEM[table.dtype], n,
+                                      ids.shape[1], ids.data_ptr(), float(scale), out.data_ptr(), _ld(out),
+                                      _stream(None)))
+    return out
+
+
+def embed_gradient(grad, ids, rows, scale=1.0, out=None, accumulate=False, dtype=None):
+    """ifvs_embed_gradient: the gradient of embed_lookup's table from `grad`,
+    the gradient of its output [n][dim].  Returns [rows][dim] in `dtype`
+    (float32 or grad's, the default); with `out` it is written there, with
+    `accumulate` added to what `out` holds."""
+    grad = _rows_arg(grad, "grad")
+    dev = grad.device
+    with _OnDevice(dev):
+        ids = _ids_arg(ids, dev)
+        n, dim = grad.shape
+        if ids.shape[0] != n:
+            raise IfvsError(E_INVALID, "ids and grad have different row counts")
+        if out is None:
+            if accumulate:
+                raise IfvsError(E_INVALID, "accumulate needs out")
+            out = torch.empty(int(rows), dim, device=dev, dtype=dtype or grad.dtype)
+        else:
+            _out_arg(out, "out", dtype or out.dtype, (int(rows), dim), dev)
+        if out.dtype not in ELEM:
+            raise IfvsError(E_INVALID, "out must be float32, float16 or bfloat16")
+        bag = ids.shape[1]
+        ws = _scratch(_lib.ifvs_embed_workspace(int(rows), dim, n, bag), dev)
+        _check(_lib.ifvs_embed_gradient(int(rows), dim, n, bag, ids.data_ptr(), float(scale), grad.data_ptr(),
+                                        _ld(grad), ELEM[grad.dtype], 1 if accumulate else 0, out.data_ptr(), _ld(out),
+                                        ELEM[out.dtype], _ptr(ws), 0 if ws is None else ws.numel(), _stream(None)))
+    return out
+
+
+def log_probs(logits, given=None, n_top=0, tau=1.0, n_valid=None):
+    """ifvs_log_probs over rows of logits [n][cols]: returns (log probability
+    of given[i][g] or None, entropy [n], top columns [n][n_top] int32 or None,
+    their log probabilities or None).  given: [n][n_given] columns; n_valid:
+    [n], only columns below it count."""
+    logits = _rows_arg(logits, "logits")
+    dev = logits.device
+    n, cols = logits.shape
+    n_top = int(n_top)
+    with _OnDevice(dev):
+        n_given = 0 if given is None else given.shape[1]
+        given = _small_arg(given, "given", torch.int32, (n, n_given), dev)
+        n_valid = _small_arg(n_valid, "n_valid", torch.int32, (n,), dev)
+        given_out = torch.empty(n, n_given, device=dev) if n_given else None
+        entropy = torch.empty(n, device=dev)
+        ids = torch.empty(n, n_top, device=dev, dtype=torch.int32) if n_top > 0 else None
+        top = torch.empty(n, n_top, device=dev) if n_top > 0 else None
+        ws = _scratch(_lib.ifvs_log_probs_workspace(n, cols, n_top), dev)
+        _check(_lib.ifvs_log_probs(n, cols, logits.data_ptr(), _ld(logits), ELEM[logits.dtype], _ptr(n_valid),
+                                   float(tau), _ptr(given), n_given, n_top, _ptr(given_out), entropy.data_ptr(),
+                                   _ptr(ids), _ptr(top), _ptr(ws), 0 if ws is None else ws.numel(), _stream(None)))
+    return given_out, entropy, ids, top
+
+
+def distill_loss(logits, teacher_ids, teacher_logits, tau=1.0, teacher_lse=None, row_weight=None, n_valid=None,
+                 want_grad=True, grad_out=None):
+    """ifvs_distill_loss: (loss [n], row_weight * dloss/dlogits or None) of
+    student logits [n][cols] against a teacher's n_teacher largest logits.
+    `grad_out` receives the gradient (it may be the logits themselves)."""
+    rows = _rows_arg(logits, "logits")
+    dev = rows.device
+    n, cols = rows.shape
+    with _OnDevice(dev):
+        k = teacher_ids.shape[1]
+        teacher_ids = _small_arg(teacher_ids, "teacher_ids", torch.int32, (n, k), dev)
+        teacher_logits = _small_arg(teacher_logits, "teacher_logits", torch.float32, (n, k), dev)
+        teacher_lse = _small_arg(teacher_lse, "teacher_lse", torch.float32, (n,), dev)
+        row_weight = _small_arg(row_weight, "row_weight", torch.float32, (n,), dev)
+        n_valid = _small_arg(n_valid, "n_valid", torch.int32, (n,), dev)
+        loss = torch.empty(n, device=dev)
+        if grad_out is not None:
+            _out_arg(grad_out, "grad_out", rows.dtype, (n, cols), dev)
+        elif want_grad:
+            grad_out = torch.empty(n, cols, device=dev, dtype=rows.dtype)
+        ws = _scratch(_lib.ifvs_distill_workspace(n, cols), dev)
+        _check(_lib.ifvs_distill_loss(n, cols, rows.data_ptr(), _ld(rows), ELEM[rows.dtype], _ptr(n_valid), k,
+                                      teacher_ids.data_ptr(), teacher_logits.data_ptr(), _ptr(teacher_lse),
+                                      float(tau), _ptr(row_weight), loss.data_ptr(), _ptr(grad_out),
+                                      cols if grad_out is None else _ld(grad_out), _ptr(ws),
+                                      0 if ws is None else ws.numel(), _stream(None)))
+    return loss, grad_out
 
 
 def bitmap_words_to_numpy(bm: torch.Tensor) -> np.ndarray:
