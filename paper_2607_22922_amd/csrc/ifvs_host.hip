@@ -2703,7 +2703,7 @@ ifvs_status ifvs_log_probs(int64_t n, int64_t cols, const void* logits, int64_t 
   a.ld = ld;
   a.dtype = dtype;
   a.n_valid = n_valid;
-  a.c = 1.4426950408889634f / tau;
+  a.c = 1.4426950408889634 / tau;
   a.given = given;
   a.n_given = n_given;
   a.n_top = n_top;
@@ -2750,7 +2750,7 @@ ifvs_status ifvs_distill_loss(int64_t n, int64_t cols, const void* logits, int64
   a.teacher_logits = teacher_logits;
   a.teacher_lse = teacher_lse;
   a.tau = tau;
-  a.c = 1.4426950408889634f / tau;
+  a.c = 1.4426950408889634 / tau;
   a.row_weight = row_weight;
   a.loss_out = loss_out;
   a.grad_out = grad_out;

@@ -588,7 +588,7 @@ struct LogProbArgs {
   int64_t ld;
   int dtype;
   const int32_t* n_valid;    // [n] or null
-  float c;                   // log2(e) / tau
+  double c;                  // log2(e) / tau
   const int32_t* given;      // [n][n_given]
   int n_given, n_top;
   float* given_out;
@@ -610,7 +610,8 @@ struct DistillArgs {
   const int32_t* teacher_ids;    // [n][n_teacher], absent outside the row
   const float* teacher_logits;   // [n][n_teacher]
   const float* teacher_lse;      // [n] or null: p is a softmax over the slots
-  float tau, c;                  // c = log2(e) / tau
+  float tau;
+  double c;                      // log2(e) / tau
   const float* row_weight;       // [n] or null (1)
   float* loss_out;               // [n]
   void* grad_out;                // [n] rows of cols, grad_ld apart; null: none; may be logits

@@ -1,11 +1,23 @@
 // Element types and row helpers of the row operators (k_embed.hip,
 // k_rows.hip): loads and stores of fp32, fp16 and bf16 rows that start at any
-// element, and fixed-order reductions over a workgroup.
+// element, a row held in registers, and reductions in a fixed order.
 #pragma once
 
 #include "ifvs_internal.h"
 
 namespace ifvs {
+
+// Sixteen bytes at any element's alignment (one global_load_dwordx4: gfx950
+// takes them unaligned).
+typedef uint32_t Word4 __attribute__((ext_vector_type(4)));
+typedef Word4 Word4At2 __attribute__((aligned(2)));
+
+__device__ __forceinline__ Word4 load_words(const void* p) {
+  return __builtin_nontemporal_load(static_cast<const Word4At2*>(p));
+}
+__device__ __forceinline__ void store_words(void* p, Word4 w) {
+  __builtin_nontemporal_store(w, static_cast<Word4At2*>(p));
+}
 
 template <typename T>
 __device__ __forceinline__ float elem_load(const T* p) {
@@ -18,42 +30,172 @@ __device__ __forceinline__ T elem_round(float v) {
   return static_cast<T>(v);
 }
 
+template <typename T>
+struct Elem;
+template <>
+struct Elem<float> {
+  static constexpr int kPerVec = 4;
+  static constexpr uint32_t kNegInfWord = 0xFF800000u;
+  static __device__ __forceinline__ void unpack(const Word4& w, float* f) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = __uint_as_float(w[j]);
+  }
+  static __device__ __forceinline__ Word4 pack(const float* f) {
+    Word4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(f[j]);
+    return w;
+  }
+};
+template <>
+struct Elem<_Float16> {
+  static constexpr int kPerVec = 8;
+  static constexpr uint32_t kNegInfWord = 0xFC00FC00u;
+  static __device__ __forceinline__ void unpack(const Word4& w, float* f) {
+    typedef _Float16 Half8 __attribute__((ext_vector_type(8)));
+    const Half8 h = __builtin_bit_cast(Half8, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = static_cast<float>(h[j]);
+  }
+  static __device__ __forceinline__ Word4 pack(const float* f) {
+    typedef _Float16 Half8 __attribute__((ext_vector_type(8)));
+    Half8 h;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = static_cast<_Float16>(f[j]);
+    return __builtin_bit_cast(Word4, h);
+  }
+};
+template <>
+struct Elem<__bf16> {
+  static constexpr int kPerVec = 8;
+  static constexpr uint32_t kNegInfWord = 0xFF80FF80u;
+  static __device__ __forceinline__ void unpack(const Word4& w, float* f) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f[2 * j] = __uint_as_float(w[j] << 16);
+      f[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+    }
+  }
+  static __device__ __forceinline__ Word4 pack(const float* f) {
+    typedef __bf16 Bf8 __attribute__((ext_vector_type(8)));
+    Bf8 h;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = static_cast<__bf16>(f[j]);
+    return __builtin_bit_cast(Word4, h);
+  }
+};
+
+// ---- reductions over a wavefront, the same value in every lane: four steps
+// on the vector unit's lane permutations (pairs, quads, eights, sixteens: no
+// LDS), then the four sixteens through scalar registers.
+template <int kCtrl>
+__device__ __forceinline__ float lane_perm(float v) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), kCtrl, 0xF, 0xF, true));
+}
+template <int kCtrl>
+__device__ __forceinline__ double lane_perm(double v) {
+  const int lo = __builtin_amdgcn_mov_dpp(__double2loint(v), kCtrl, 0xF, 0xF, true);
+  const int hi = __builtin_amdgcn_mov_dpp(__double2hiint(v), kCtrl, 0xF, 0xF, true);
+  return __hiloint2double(hi, lo);
+}
+constexpr int kPermXor1 = 0xB1, kPermXor2 = 0x4E, kPermHalfMirror = 0x141, kPermMirror = 0x140;
+
+__device__ __forceinline__ float lane_of(float v, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+__device__ __forceinline__ double lane_of(double v, int lane) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane),
+                          __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
+
+__device__ __forceinline__ float quad_max(float v) {
+  v = fmaxf(v, lane_perm<kPermXor1>(v));
+  return fmaxf(v, lane_perm<kPermXor2>(v));
+}
+__device__ __forceinline__ float sixteen_max(float v) {
+  v = quad_max(v);
+  v = fmaxf(v, lane_perm<kPermHalfMirror>(v));
+  return fmaxf(v, lane_perm<kPermMirror>(v));
+}
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  return v;
+  v = sixteen_max(v);
+  return fmaxf(fmaxf(lane_of(v, 0), lane_of(v, 16)), fmaxf(lane_of(v, 32), lane_of(v, 48)));
 }
-
 __device__ __forceinline__ double wave_add(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+  v += lane_perm<kPermXor1>(v);
+  v += lane_perm<kPermXor2>(v);
+  v += lane_perm<kPermHalfMirror>(v);
+  v += lane_perm<kPermMirror>(v);
+  return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
+}
+__device__ __forceinline__ double wave_max(double v) {
+  v = fmax(v, lane_perm<kPermXor1>(v));
+  v = fmax(v, lane_perm<kPermXor2>(v));
+  v = fmax(v, lane_perm<kPermHalfMirror>(v));
+  v = fmax(v, lane_perm<kPermMirror>(v));
+  return fmax(fmax(lane_of(v, 0), lane_of(v, 16)), fmax(lane_of(v, 32), lane_of(v, 48)));
 }
 
-// Sum / maximum over the workgroup, the same value in every thread; `s` holds
-// one entry per wavefront and may be reused right after the call.
-template <int kWaves>
-__device__ __forceinline__ double block_add(double v, double* s) {
-  v = wave_add(v);
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = 0.0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) v += s[w];
-  __syncthreads();
-  return v;
+// A barrier that a workgroup of one wavefront does not need: its own LDS
+// operations stay in order.
+template <int kThreads>
+__device__ __forceinline__ void group_sync() {
+  if constexpr (kThreads > 64) {
+    __syncthreads();
+  } else {
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
 }
 
-template <int kWaves>
-__device__ __forceinline__ float block_max(float v, double* s) {
-  v = wave_max(v);
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = -INFINITY;
+// Up to kThreads * kVecs vectors and a tail of less than one vector of a row,
+// in the registers of a workgroup: thread t holds vectors t, t + kThreads, ...
+// and element t of the tail; places past the end hold -inf.  Loops step over
+// vector rounds that lie wholly past the end.
+template <typename T, int kThreads, int kVecs>
+struct RowTile {
+  static constexpr int kE = Elem<T>::kPerVec;
+  static constexpr int kCapacity = kThreads * kVecs * kE;
+  Word4 v[kVecs];
+  float tail;
+  int nvec, ntail;
+
+  __device__ __forceinline__ void load(const T* x, int len) {
+    const int tid = threadIdx.x;
+    nvec = len / kE;
+    ntail = len - nvec * kE;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) v = fmaxf(v, static_cast<float>(s[w]));
-  __syncthreads();
-  return v;
-}
+    for (int i = 0; i < kVecs; ++i) {
+      const int at = i * kThreads + tid;
+      v[i] = Word4{Elem<T>::kNegInfWord, Elem<T>::kNegInfWord, Elem<T>::kNegInfWord, Elem<T>::kNegInfWord};
+      if (at < nvec) v[i] = load_words(reinterpret_cast<const char*>(x) + static_cast<uint32_t>(at) * 16u);
+    }
+    tail = tid < ntail ? elem_load(x + nvec * kE + tid) : -INFINITY;
+  }
+  __device__ __forceinline__ bool has(int i) const { return i * kThreads < nvec; }
+  __device__ __forceinline__ int column(int i, int j) const { return (i * kThreads + static_cast<int>(threadIdx.x)) * kE + j; }
+  __device__ __forceinline__ int tail_column() const { return nvec * kE + static_cast<int>(threadIdx.x); }
+
+  // Between two passes over the tile: the compiler would keep every unpacked
+  // element of the first alive for the second (two to three times the registers).
+  __device__ __forceinline__ void forget_unpacked() {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) asm volatile("" : "+v"(v[i]));
+  }
+
+  // Maximum of the thread's elements (NaN ones are passed over).
+  __device__ __forceinline__ float thread_max() const {
+    float m = tail;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+      if (has(i)) {
+        float f[kE];
+        Elem<T>::unpack(v[i], f);
+#pragma unroll
+        for (int j = 0; j < kE; j += 2) m = fmaxf(fmaxf(m, f[j]), f[j + 1]);
+      }
+    return m;
+  }
+};
 
 }  // namespace ifvs
