@@ -369,168 +369,437 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(const LogProbArgs a,
 }
 
 // ------------------------------------------------------------- distillation
-// One workgroup per row.  The teacher's probabilities are held in LDS; a
-// column's teacher probability is looked up among the slots.
-constexpr int kRowThreads = 256;
-constexpr int kRowWaves = kRowThreads / 64;
-
-struct RowRef {
-  float c;       // log2(e) / tau
-  float shift;   // subtracted before the product (0, or the maximum)
-  float b;       // subtracted after it
-  __device__ __forceinline__ float exponent(float x) const { return __fmaf_rn(x - shift, c, -b); }
-  __device__ __forceinline__ double exponent64(float x) const {
-    return (static_cast<double>(x) - shift) * c - b;
-  }
-  // What an exponent is relative to: x c = exponent + origin.
-  __device__ __forceinline__ double origin() const { return static_cast<double>(shift) * c + b; }
+// A row's columns are those that teacher slots name ("named", at most
+// n_teacher) and the others.  The others' sum comes from the tile, with the
+// named columns taken out of it before (a bit per column in LDS); the named
+// ones are computed one by one in 64 bits.  So the rest's share is summed by
+// itself, never as a difference, and a teacher that takes nearly everything
+// loses no bits.  With R the others' log2 sum and L the row's, an other
+// column's gradient is
+//   weight tau (q - P q / Q) = [weight tau (2^(R - L) - P)] 2^(x c - R):
+// one exponential and one product a column, for both forms of the loss (P = 0
+// without teacher_lse).
+//
+// The loss is a difference of logarithms that may be 1e-3 of them, so the
+// exponents are computed with c in two parts (log2(e) / tau rounded to fp32
+// alone moves the temperature by 2^-25).  c_lo > 0, so that -inf stays -inf.
+struct SplitC {
+  float hi, lo;
 };
 
-__device__ __forceinline__ RowRef row_ref(float mx, float c) {
-  const float b = mx * c;
-  if (fabsf(b) < 1e37f) return {c, 0.0f, b};
-  return {c, mx, 0.0f};
+__device__ __forceinline__ SplitC split_c(double c) {
+  float hi = static_cast<float>(c);
+  if (hi >= c) hi = __uint_as_float(__float_as_uint(hi) - 1);
+  return {hi, static_cast<float>(c - hi)};
 }
 
-template <int kWaves>
-__device__ __forceinline__ double block_add(double v, double* s) {
-  v = wave_add(v);
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = 0.0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) v += s[w];
-  __syncthreads();
-  return v;
+// A chunk's sums: the others', relative to 2^other_origin, and the named
+// columns', relative to 2^named_origin; over the named slots sum p (log p -
+// ln 2 (x c - named_origin)) and sum p.  named_sum is NaN where the row has no
+// finite distribution or no finite teacher.
+struct DistillStat {
+  double other_origin, other_sum, named_origin, named_sum, loss, psum;
+};
+
+// What the row's gradient needs: an other column has coef 2^(x c - origin), a
+// named one weight tau (2^(x c - origin - lse2) - p).
+constexpr int kRowNan = 1, kRowFinite = 2;        // 0: loss and gradient 0
+struct DistillRow {
+  double origin, lse2;
+  float coef, loss;
+  int mode;
+};
+
+// Dynamic LDS of the distillation: per slot the column relative to the chunk
+// (-1 elsewhere), the probabilities and the logit; then a bit per column.
+struct TeacherLds {
+  double* p;
+  float* x;
+  int* column;
+  unsigned char* bits;
+};
+
+__device__ __forceinline__ TeacherLds teacher_lds(unsigned char* smem, int n_teacher) {
+  TeacherLds t;
+  t.p = reinterpret_cast<double*>(smem);
+  t.x = reinterpret_cast<float*>(t.p + n_teacher);
+  t.column = reinterpret_cast<int*>(t.x + n_teacher);
+  t.bits = smem + ((static_cast<size_t>(n_teacher) * 16 + 8 + 15) & ~size_t{15});
+  return t;
 }
 
-template <int kWaves>
-__device__ __forceinline__ float block_max(float v, double* s) {
-  v = wave_max(v);
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = -INFINITY;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) v = fmaxf(v, static_cast<float>(s[w]));
-  __syncthreads();
-  return v;
-}
+// What one wavefront finds out about the teacher.
+struct Teacher {
+  double lse;          // natural logarithm of its sum
+  double rest;         // P
+  bool bad, present;
+};
 
-template <typename T>
-__global__ __launch_bounds__(kRowThreads) void distill_kernel(const DistillArgs a) {
-  extern __shared__ __align__(16) unsigned char smem[];
-  double* s_red = reinterpret_cast<double*>(smem);          // [kRowWaves]
-  double* s_p = s_red + kRowWaves;                            // [n_teacher]
-  int* s_id = reinterpret_cast<int*>(s_p + a.n_teacher);      // [n_teacher], -1 absent
-  const int tid = threadIdx.x;
-  const int64_t i = blockIdx.x;
-  const T* x = static_cast<const T*>(a.logits) + i * a.ld;
-  T* grad = a.grad_out ? static_cast<T*>(a.grad_out) + i * a.grad_ld : nullptr;
-  const int cols = static_cast<int>(a.cols);
-  const float weight = a.row_weight ? a.row_weight[i] : 1.0f;
-  const int len = row_cols(a.n_valid, i, a.cols);
-  auto skip = [&](float loss, float g) {
-    if (tid == 0) a.loss_out[i] = loss;
-    if (grad)
-      for (int v = tid; v < cols; v += kRowThreads) grad[v] = elem_round<T>(v < len ? g : 0.0f);
-  };
-  if (weight == 0.0f) return skip(0.0f, 0.0f);
-
-  // The teacher.
+// One wavefront reads the slots; columns in [first, first + mine) are named.
+__device__ __forceinline__ Teacher read_teacher(const DistillArgs& a, int64_t row, int len, int first, int mine,
+                                                const TeacherLds& t) {
+  const int lane = threadIdx.x & 63;
+  const int32_t* ids = a.teacher_ids + row * a.n_teacher;
+  const float* logits = a.teacher_logits + row * a.n_teacher;
   const double inv_tau = 1.0 / static_cast<double>(a.tau);
-  float tmax = -INFINITY;
-  double bad = 0.0, present = 0.0;
-  for (int k = tid; k < a.n_teacher; k += kRowThreads) {
-    const int id = a.teacher_ids[i * a.n_teacher + k];
-    const float t = a.teacher_logits[i * a.n_teacher + k];
-    const bool there = id >= 0 && id < len;
-    s_id[k] = there ? id : -1;
-    if (!there) continue;
-    present += 1.0;
-    if (isnan(t) || t == INFINITY) bad = 1.0;
-    tmax = fmaxf(tmax, t);
+  float mx = -INFINITY;
+  bool bad = false, present = false;
+  for (int k = lane; k < a.n_teacher; k += 64) {
+    const int id = ids[k];
+    const float v = logits[k];
+    if (id >= 0 && id < len) {
+      present = true;
+      if (isnan(v) || v == INFINITY) bad = true;
+      mx = fmaxf(mx, v);
+    }
+    t.column[k] = id >= first && id < first + mine ? id - first : -1;
   }
-  present = block_add<kRowWaves>(present, s_red);
-  const bool rest = a.teacher_lse != nullptr;
-  double lse;
-  if (rest) {
-    lse = a.teacher_lse[i];
+  Teacher out;
+  out.present = __any(present);
+  mx = wave_max(mx);
+  if (a.teacher_lse) {
+    out.lse = a.teacher_lse[row];
   } else {
-    tmax = block_max<kRowWaves>(tmax, s_red);
+    if (out.present && mx == -INFINITY) bad = true;
     double sum = 0.0;
-    for (int k = tid; k < a.n_teacher; k += kRowThreads)
-      if (s_id[k] >= 0) sum += exp((static_cast<double>(a.teacher_logits[i * a.n_teacher + k]) - tmax) * inv_tau);
-    sum = block_add<kRowWaves>(sum, s_red);
-    lse = static_cast<double>(tmax) * inv_tau + log(sum);
-    if (present > 0.0 && tmax == -INFINITY) bad = 1.0;
+    for (int k = lane; k < a.n_teacher; k += 64)
+      if (ids[k] >= 0 && ids[k] < len) sum += exp((static_cast<double>(logits[k]) - mx) * inv_tau);
+    out.lse = mx * inv_tau + log(wave_add(sum));
   }
   double psum = 0.0;
-  for (int k = tid; k < a.n_teacher; k += kRowThreads) {
-    const double p =
-        s_id[k] < 0 ? 0.0 : exp(static_cast<double>(a.teacher_logits[i * a.n_teacher + k]) * inv_tau - lse);
-    s_p[k] = p;
+  for (int k = lane; k < a.n_teacher; k += 64) {
+    const double p = ids[k] >= 0 && ids[k] < len ? exp(logits[k] * inv_tau - out.lse) : 0.0;
+    t.p[k] = p;
     psum += p;
   }
-  psum = block_add<kRowWaves>(psum, s_red);
-  const double p_rest = rest ? fmax(0.0, 1.0 - psum) : 0.0;
+  out.rest = a.teacher_lse ? fmax(0.0, 1.0 - wave_add(psum)) : 0.0;
+  out.bad = __any(bad);
+  return out;
+}
 
-  // The student: all columns, and those that no slot names.
-  auto named = [&](int v) {
-    for (int k = 0; k < a.n_teacher; ++k)
-      if (s_id[k] == v) return true;
-    return false;
-  };
-  float mx = -INFINITY, mx_rest = -INFINITY;
-  for (int v = tid; v < len; v += kRowThreads) {
-    const float f = elem_load(x + v);
-    if (isnan(f) || f == INFINITY) bad = 1.0;
-    mx = fmaxf(mx, f);
-    if (rest && !named(v)) mx_rest = fmaxf(mx_rest, f);
-  }
-  bad = block_add<kRowWaves>(bad, s_red);
-  mx = block_max<kRowWaves>(mx, s_red);
-  mx_rest = block_max<kRowWaves>(mx_rest, s_red);
-  if (bad > 0.0) return skip(NAN, NAN);
-  if (mx == -INFINITY || (!rest && present == 0.0)) return skip(0.0f, 0.0f);
-  const RowRef ref = row_ref(mx, static_cast<float>(a.c)), ref_rest = row_ref(mx_rest, static_cast<float>(a.c));
-  float sum = 0.0f, sum_rest = 0.0f;
-  for (int v = tid; v < len; v += kRowThreads) {
-    const float f = elem_load(x + v);
-    sum += exp2f(ref.exponent(f));
-    if (rest && mx_rest > -INFINITY && !named(v)) sum_rest += exp2f(ref_rest.exponent(f));
-  }
-  const double S = block_add<kRowWaves>(sum, s_red);
-  const double S_rest = block_add<kRowWaves>(sum_rest, s_red);
-  const double log2S = log2(S);
+// 2^d of a difference of exponents.
+__device__ __forceinline__ double pow2(double d) { return d < -4000.0 ? 0.0 : exp2(d); }
 
-  double loss = 0.0;
-  for (int k = tid; k < a.n_teacher; k += kRowThreads)
-    if (s_id[k] >= 0 && s_p[k] > 0.0)
-      loss += s_p[k] * (log(s_p[k]) - (ref.exponent64(elem_load(x + s_id[k])) - log2S) * kLn2);
-  loss = block_add<kRowWaves>(loss, s_red);
-  // log Q of the rest, relative to the row's own sum.
-  const double logQ = S_rest > 0.0 ? (ref_rest.origin() - ref.origin() + log2(S_rest) - log2S) * kLn2 : -INFINITY;
-  if (p_rest > 0.0 && S_rest > 0.0) loss += p_rest * (log(p_rest) - logQ);
-  if (tid == 0) a.loss_out[i] = static_cast<float>(loss * (static_cast<double>(a.tau) * a.tau));
-  if (!grad) return;
-  __syncthreads();                       // the listed logits are read: in place from here on
-  const double up = static_cast<double>(weight) * a.tau;
-  const double keep = rest && S_rest > 0.0 ? 1.0 - p_rest * exp(-logQ) : 1.0;
-  for (int v = tid; v < cols; v += kRowThreads) {
-    double g = 0.0;
-    if (v < len) {
-      const double q = exp2(ref.exponent64(elem_load(x + v)) - log2S);
-      double p = 0.0;
-      bool is_named = false;
-      for (int k = 0; k < a.n_teacher; ++k)
-        if (s_id[k] == v) {
-          p += s_p[k];
-          is_named = true;
-        }
-      g = up * (rest && !is_named ? q * keep : q - p);
+// The named columns' part of a chunk's sums, by one wavefront.  A column that
+// several slots name counts once in the student's sum.
+__device__ __forceinline__ DistillStat named_stat(const DistillArgs& a, int64_t row, const TeacherLds& t,
+                                                  const Teacher& teacher) {
+  const int lane = threadIdx.x & 63;
+  const double inv_tau = 1.0 / static_cast<double>(a.tau);
+  const float* logits = a.teacher_logits + row * a.n_teacher;
+  double mx = -INFINITY;
+  bool bad = teacher.bad;
+  for (int k = lane; k < a.n_teacher; k += 64)
+    if (t.column[k] >= 0) {
+      const float x = t.x[k];
+      if (isnan(x) || x == INFINITY) bad = true;
+      mx = fmax(mx, x * a.c);
     }
-    grad[v] = elem_round<T>(static_cast<float>(g));
+  mx = wave_max(mx);
+  if (mx == -INFINITY) mx = 0.0;
+  double sum = 0.0, loss = 0.0, psum = 0.0;
+  for (int k = lane; k < a.n_teacher; k += 64) {
+    const int column = t.column[k];
+    if (column < 0) continue;
+    const double z = t.x[k] * a.c - mx, p = t.p[k];
+    bool again = false;
+    for (int o = 0; o < k; ++o) again |= t.column[o] == column;
+    if (!again) sum += pow2(z);
+    if (p > 0.0) {
+      loss += p * (logits[k] * inv_tau - teacher.lse - z * kLn2);
+      psum += p;
+    }
   }
+  sum = wave_add(sum);
+  return {0.0, 0.0, mx, __any(bad) ? NAN : sum, wave_add(loss), wave_add(psum)};
+}
+
+// Joins the statistics that a wavefront's first `count` lanes hold, in every lane.
+__device__ __forceinline__ DistillStat join_lanes(DistillStat st, int count) {
+  const int lane = threadIdx.x & 63;
+  const bool other = lane < count && st.other_sum != 0.0;
+  const double o = wave_max(other ? st.other_origin : -INFINITY);
+  st.other_sum = wave_add(other ? times_pow2(st.other_sum, st.other_origin - o) : 0.0);
+  st.other_origin = o;
+  const bool named = lane < count && (st.named_sum != 0.0 || st.psum != 0.0);
+  const double m = wave_max(named ? st.named_origin : -INFINITY);
+  const double d = named ? st.named_origin - m : 0.0;
+  // sum p (log p - ln 2 (x c - m)) from the chunk's own origin
+  st.loss = wave_add(named ? (st.psum == 0.0 ? 0.0 : st.loss - st.psum * d * kLn2) : 0.0);
+  st.named_sum = wave_add(named ? st.named_sum * pow2(d) : 0.0);
+  st.psum = wave_add(named ? st.psum : 0.0);
+  st.named_origin = m;
+  return st;
+}
+
+// From the whole row's sums: its loss, and what the gradient needs.
+__device__ __forceinline__ DistillRow distill_row(const DistillArgs& a, const DistillStat& st, const Teacher& teacher,
+                                                  float weight) {
+  DistillRow r{};
+  if (!a.teacher_lse && !teacher.present) return r;                   // nothing to follow
+  const bool other = st.other_sum != 0.0, named = st.named_sum != 0.0;
+  if (teacher.bad || isnan(st.other_sum) || isnan(st.named_sum)) {
+    r.mode = kRowNan;
+    r.loss = NAN;
+    return r;
+  }
+  if (!other && !named) return r;                                     // no distribution
+  const double hi = fmax(other ? st.other_origin : -INFINITY, named ? st.named_origin : -INFINITY);
+  const double all = (other ? st.other_sum * pow2(st.other_origin - hi) : 0.0) +
+                     (named ? st.named_sum * pow2(st.named_origin - hi) : 0.0);
+  r.mode = kRowFinite;
+  r.origin = other ? st.other_origin : hi;
+  const double log2_all = log2(all);
+  r.lse2 = (hi - r.origin) + log2_all;
+  double loss = st.psum > 0.0 ? st.loss + st.psum * ((hi - st.named_origin) + log2_all) * kLn2 : 0.0;
+  if (other) {
+    const double log2_q = log2(st.other_sum) - r.lse2;                // of the others' share Q
+    if (teacher.rest > 0.0) loss += teacher.rest * (log(teacher.rest) - log2_q * kLn2);
+    r.coef = static_cast<float>(static_cast<double>(weight) * a.tau * (exp2(log2_q) - teacher.rest) / st.other_sum);
+  }
+  r.loss = static_cast<float>(loss * (static_cast<double>(a.tau) * a.tau));
+  return r;
+}
+
+// The other columns' sum in a wavefront's registers, in every lane.
+template <typename T, int kThreads, int kVecs>
+__device__ __forceinline__ void other_stat(RowTile<T, kThreads, kVecs>& tile, float mx, const DistillArgs& a,
+                                           DistillStat& st) {
+  constexpr int kE = Elem<T>::kPerVec;
+  const SplitC c = split_c(a.c);
+  const float b = mx == -INFINITY ? 0.0f : rintf(mx * c.hi);
+  float sum = 0.0f;
+  auto each = [&](auto&& add) {
+    tile.forget_unpacked();
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+      if (tile.has(i)) {
+        float f[kE];
+        Elem<T>::unpack(tile.v[i], f);
+#pragma unroll
+        for (int j = 0; j < kE; ++j) add(f[j]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    add(tile.tail);
+  };
+  if (fabsf(b) < kHuge) {
+    st.other_origin = b;
+    each([&](float x) { sum += exp2_fast(__fmaf_rn(x, c.lo, __fmaf_rn(x, c.hi, -b))); });
+  } else {
+    st.other_origin = mx * a.c;
+    each([&](float x) { sum += x == mx ? 1.0f : (isnan(x) ? NAN : 0.0f); });
+    if (mx == INFINITY) sum = NAN;
+  }
+  st.other_sum = wave_add(static_cast<double>(sum));
+}
+
+// n elements of g at p.
+template <typename T>
+__device__ __forceinline__ void fill_range(T* p, int n, float g, int tid, int threads) {
+  constexpr int kE = Elem<T>::kPerVec;
+  float f[kE];
+#pragma unroll
+  for (int j = 0; j < kE; ++j) f[j] = g;
+  const Word4 w = Elem<T>::pack(f);
+  const int nvec = n / kE;
+  for (int v = tid; v < nvec; v += threads) store_words(p + v * kE, w);
+  for (int v = nvec * kE + tid; v < n; v += threads) p[v] = elem_round<T>(g);
+}
+
+// The gradient of a chunk: `mine` columns of the tile, zeros up to `cols`.
+// Every column is written as another one, then, after a barrier, the named
+// ones anew (wave stores to one address stay in order once they have left).
+template <typename T, int kThreads, int kVecs>
+__device__ __forceinline__ void write_gradient(RowTile<T, kThreads, kVecs>& tile, const DistillArgs& a,
+                                               const DistillRow& r, float weight, const TeacherLds& t, T* grad, int mine,
+                                               int cols) {
+  constexpr int kE = Elem<T>::kPerVec;
+  const int tid = threadIdx.x;
+  fill_range(grad + mine, cols - mine, 0.0f, tid, kThreads);
+  if (r.mode != kRowFinite) {
+    fill_range(grad, mine, r.mode == kRowNan ? NAN : 0.0f, tid, kThreads);
+    return;
+  }
+  const SplitC c = split_c(a.c);
+  const float coef = r.coef;
+  auto each = [&](auto&& fn) {
+    tile.forget_unpacked();
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+      if (tile.has(i)) {
+        const int at = i * kThreads + tid;
+        if (at < tile.nvec) {
+          float f[kE];
+          Elem<T>::unpack(tile.v[i], f);
+#pragma unroll
+          for (int j = 0; j < kE; ++j) f[j] = fn(f[j]);
+          store_words(reinterpret_cast<char*>(grad) + static_cast<uint32_t>(at) * 16u, Elem<T>::pack(f));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    if (tid < tile.ntail) grad[tile.tail_column()] = elem_round<T>(fn(tile.tail));
+  };
+  if (fabs(r.origin) < kHuge) {
+    const float b = static_cast<float>(r.origin);
+    each([&](float x) { return coef * exp2_fast(__fmaf_rn(x, c.lo, __fmaf_rn(x, c.hi, -b))); });
+  } else {
+    each([&](float x) { return x * a.c == r.origin ? coef : 0.0f; });
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  group_sync<kThreads>();
+  for (int k = tid; k < a.n_teacher; k += kThreads) {
+    const int column = t.column[k];
+    if (column < 0) continue;
+    double p = 0.0;
+    for (int o = 0; o < a.n_teacher; ++o) p += t.column[o] == column ? t.p[o] : 0.0;
+    const double q = pow2(t.x[k] * a.c - r.origin - r.lse2);
+    grad[column] = elem_round<T>(static_cast<float>(static_cast<double>(weight) * a.tau * (q - p)));
+  }
+}
+
+// The chunk's named columns' logits and bits, by the wavefront that read the
+// teacher; bits may be null.
+template <typename T>
+__device__ __forceinline__ void gather_named(const DistillArgs& a, const T* x, const TeacherLds& t) {
+  for (int k = threadIdx.x & 63; k < a.n_teacher; k += 64) {
+    const int column = t.column[k];
+    t.x[k] = column >= 0 ? elem_load(x + column) : -INFINITY;
+  }
+}
+
+// Takes the named columns out of the tile.
+template <typename T, int kThreads, int kVecs>
+__device__ __forceinline__ void drop_named(RowTile<T, kThreads, kVecs>& tile, const unsigned char* bits) {
+  constexpr int kE = Elem<T>::kPerVec;
+  const int tid = threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i)
+    if (tile.has(i)) {
+      const uint32_t hit = bits[i * kThreads + tid];
+      if (hit != 0) {
+        float f[kE];
+        Elem<T>::unpack(tile.v[i], f);
+#pragma unroll
+        for (int j = 0; j < kE; ++j) f[j] = (hit >> j) & 1u ? -INFINITY : f[j];
+        tile.v[i] = Elem<T>::pack(f);
+      }
+    }
+  if (tid < tile.ntail && ((bits[tile.nvec] >> tid) & 1u)) tile.tail = -INFINITY;
+}
+
+// One workgroup per row (kWhole: chunks is 1, loss and gradient are written)
+// or per (row, chunk), whose sums go to the workspace.
+template <typename T, int kThreads, int kVecs, bool kWhole>
+__global__ __launch_bounds__(kThreads, 4) void distill_tile_kernel(
+    const DistillArgs a, int64_t item0, int chunk, int chunks, DistillStat* stats) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int kWaves = kThreads / 64;
+  __shared__ DistillStat s_stat[kWaves];
+  __shared__ DistillRow s_row;
+  const int tid = threadIdx.x;
+  const int64_t item = item0 + blockIdx.x;
+  const int64_t row = kWhole ? item : item / chunks;
+  const int first = kWhole ? 0 : static_cast<int>(item - row * chunks) * chunk;
+  const float weight = a.row_weight ? a.row_weight[row] : 1.0f;
+  const int cols = static_cast<int>(a.cols);
+  if (weight == 0.0f) {
+    if constexpr (kWhole) {
+      if (tid == 0) a.loss_out[row] = 0.0f;
+      if (a.grad_out) fill_range(static_cast<T*>(a.grad_out) + row * a.grad_ld, cols, 0.0f, tid, kThreads);
+    }
+    return;
+  }
+  const T* x = static_cast<const T*>(a.logits) + row * a.ld + first;
+  const int len = row_cols(a.n_valid, row, a.cols);
+  const int mine = kWhole ? len : max(0, min(chunk, len - first));
+  const TeacherLds t = teacher_lds(smem, a.n_teacher);
+  RowTile<T, kThreads, kVecs> tile;
+  tile.load(x, mine);
+  Teacher teacher{};
+  DistillStat st{};
+  if (tid < 64) {
+    constexpr int kBitWords = (kThreads * kVecs + 16) / 16;
+    for (int w = tid; w < kBitWords; w += 64) reinterpret_cast<Word4*>(t.bits)[w] = Word4{0, 0, 0, 0};
+    teacher = read_teacher(a, row, len, first, mine, t);
+    gather_named(a, x, t);
+    for (int k = tid; k < a.n_teacher; k += 64) {
+      const int column = t.column[k];
+      if (column >= 0) {
+        const int vec = column / Elem<T>::kPerVec;
+        atomicOr(reinterpret_cast<unsigned*>(t.bits) + (vec >> 2), 1u << (8 * (vec & 3) + column % Elem<T>::kPerVec));
+      }
+    }
+    st = named_stat(a, row, t, teacher);
+  }
+  group_sync<kThreads>();
+  drop_named(tile, t.bits);
+  DistillStat mine_st{};
+  other_stat(tile, wave_max(tile.thread_max()), a, mine_st);
+  if constexpr (kWaves > 1) {
+    if ((tid & 63) == 0) s_stat[tid >> 6] = mine_st;
+    __syncthreads();
+  }
+  if (tid < 64) {
+    if constexpr (kWaves > 1) mine_st = join_lanes(tid < kWaves ? s_stat[tid] : DistillStat{}, kWaves);
+    st.other_origin = mine_st.other_origin;
+    st.other_sum = mine_st.other_sum;
+    if constexpr (kWhole) {
+      const DistillRow r = distill_row(a, st, teacher, weight);
+      if (tid == 0) {
+        s_row = r;
+        a.loss_out[row] = r.loss;
+      }
+    } else if (tid == 0) {
+      stats[item] = st;
+    }
+  }
+  if constexpr (kWhole) {
+    if (!a.grad_out) return;
+    group_sync<kThreads>();
+    write_gradient(tile, a, s_row, weight, t, static_cast<T*>(a.grad_out) + row * a.grad_ld, mine, cols);
+  }
+}
+
+// The second launch of rows in chunks: every workgroup joins its row's sums
+// and writes its chunk's gradient, the first chunk's also the loss.  Without a
+// gradient one wavefront per row (chunks_grid 1).
+template <typename T, int kThreads, int kVecs>
+__global__ __launch_bounds__(kThreads) void distill_join_kernel(const DistillArgs a, int64_t item0, int chunk,
+                                                                int chunks, int chunks_grid,
+                                                                const DistillStat* stats) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ DistillRow s_row;
+  const int tid = threadIdx.x;
+  const int64_t item = item0 + blockIdx.x;
+  const int64_t row = item / chunks_grid;
+  const int first = static_cast<int>(item - row * chunks_grid) * chunk;
+  const float weight = a.row_weight ? a.row_weight[row] : 1.0f;
+  const int cols = min(chunk, static_cast<int>(a.cols) - first);
+  T* grad = a.grad_out ? static_cast<T*>(a.grad_out) + row * a.grad_ld + first : nullptr;
+  if (weight == 0.0f) {
+    if (first == 0 && tid == 0) a.loss_out[row] = 0.0f;
+    if (grad) fill_range(grad, cols, 0.0f, tid, kThreads);
+    return;
+  }
+  const T* x = static_cast<const T*>(a.logits) + row * a.ld + first;
+  const int len = row_cols(a.n_valid, row, a.cols);
+  const int mine = max(0, min(chunk, len - first));
+  const TeacherLds t = teacher_lds(smem, a.n_teacher);
+  RowTile<T, kThreads, kVecs> tile;
+  if (grad) tile.load(x, mine);
+  if (tid < 64) {
+    const DistillStat own = tid < chunks ? stats[row * chunks + tid] : DistillStat{};
+    const Teacher teacher = read_teacher(a, row, len, first, mine, t);
+    if (grad) gather_named(a, x, t);
+    const DistillRow r = distill_row(a, join_lanes(own, chunks), teacher, weight);
+    if (tid == 0) {
+      s_row = r;
+      if (first == 0) a.loss_out[row] = r.loss;
+    }
+  }
+  if (!grad) return;
+  group_sync<kThreads>();
+  write_gradient(tile, a, s_row, weight, t, grad, mine, cols);
 }
 
 }  // namespace
@@ -566,8 +835,6 @@ int64_t log_probs_workspace_bytes(int64_t n, int64_t cols, int n_top) {
   }
   return most * static_cast<int64_t>(sizeof(Stat) + 8 * n_top);
 }
-int64_t distill_workspace_bytes(int64_t, int64_t) { return 0; }
-
 // Launches fn(first item, items) over slices that a grid can count.
 template <typename F>
 hipError_t in_slices(int64_t items, F&& fn) {
@@ -611,16 +878,60 @@ hipError_t launch_log_probs(const LogProbArgs& a, hipStream_t s) {
   }
 }
 
-hipError_t launch_distill(const DistillArgs& a, hipStream_t s) {
-  if (a.n == 0) return hipSuccess;
-  const dim3 grid(static_cast<unsigned>(a.n)), block(kRowThreads);
-  const size_t lds = sizeof(double) * kRowWaves + (sizeof(double) + sizeof(int)) * a.n_teacher;
-  switch (a.dtype) {
-    case kElemF32: distill_kernel<float><<<grid, block, lds, s>>>(a); break;
-    case kElemF16: distill_kernel<_Float16><<<grid, block, lds, s>>>(a); break;
-    default: distill_kernel<__bf16><<<grid, block, lds, s>>>(a); break;
+// As log_probs_plan, and rows of up to 16384 vectors to one workgroup of 1024
+// threads: it reads the logits once, where two launches read them twice.
+RowPlan distill_plan(int64_t n, int64_t cols, int per_vec) {
+  const int64_t vecs = (cols + per_vec - 1) / per_vec;
+  if (vecs > 4096 && vecs <= 16384 && n >= 128) return {1024, 16, static_cast<int>(cols), 1};
+  return log_probs_plan(n, cols, per_vec);
+}
+
+int64_t distill_workspace_bytes(int64_t n, int64_t cols) {
+  int64_t most = 0;                            // the element type is not known here
+  for (int per_vec : {4, 8}) {
+    const RowPlan p = distill_plan(n, cols, per_vec);
+    if (n > 0 && p.chunks > 1) most = std::max<int64_t>(most, n * p.chunks);
   }
-  return hipGetLastError();
+  return most * static_cast<int64_t>(sizeof(DistillStat));
+}
+
+template <typename T>
+hipError_t distill_typed(const DistillArgs& a, hipStream_t s) {
+  const RowPlan p = distill_plan(a.n, a.cols, Elem<T>::kPerVec);
+  DistillStat* stats = static_cast<DistillStat*>(a.workspace);
+  const size_t slots = static_cast<size_t>(a.n_teacher) * 16 + 8;
+  const size_t lds = ((slots + 15) & ~size_t{15}) + static_cast<size_t>(p.threads) * p.vecs + 16;
+  const int64_t items = a.n * p.chunks;
+  const hipError_t e = in_slices(items, [&](int64_t at, unsigned grid) {
+    if (p.chunks > 1) {
+      if (p.vecs == 8) distill_tile_kernel<T, 256, 8, false><<<grid, 256, lds, s>>>(a, at, p.chunk, p.chunks, stats);
+      else distill_tile_kernel<T, 256, 16, false><<<grid, 256, lds, s>>>(a, at, p.chunk, p.chunks, stats);
+    } else if (p.threads == 64) {
+      if (p.vecs == 2) distill_tile_kernel<T, 64, 2, true><<<grid, 64, lds, s>>>(a, at, p.chunk, 1, stats);
+      else distill_tile_kernel<T, 64, 8, true><<<grid, 64, lds, s>>>(a, at, p.chunk, 1, stats);
+    } else if (p.threads == 256) {
+      if (p.vecs == 8) distill_tile_kernel<T, 256, 8, true><<<grid, 256, lds, s>>>(a, at, p.chunk, 1, stats);
+      else distill_tile_kernel<T, 256, 16, true><<<grid, 256, lds, s>>>(a, at, p.chunk, 1, stats);
+    } else {
+      distill_tile_kernel<T, 1024, 16, true><<<grid, 1024, lds, s>>>(a, at, p.chunk, 1, stats);
+    }
+  });
+  if (e != hipSuccess || p.chunks == 1) return e;
+  const int per_row = a.grad_out ? p.chunks : 1;
+  return in_slices(a.n * per_row, [&](int64_t at, unsigned grid) {
+    if (!a.grad_out) distill_join_kernel<T, 64, 2><<<grid, 64, slots, s>>>(a, at, p.chunk, p.chunks, 1, stats);
+    else if (p.vecs == 8) distill_join_kernel<T, 256, 8><<<grid, 256, slots, s>>>(a, at, p.chunk, p.chunks, per_row, stats);
+    else distill_join_kernel<T, 256, 16><<<grid, 256, slots, s>>>(a, at, p.chunk, p.chunks, per_row, stats);
+  });
+}
+
+hipError_t launch_distill(const DistillArgs& a, hipStream_t s) {
+  switch (a.n == 0 ? -1 : a.dtype) {
+    case -1: return hipSuccess;
+    case kElemF32: return distill_typed<float>(a, s);
+    case kElemF16: return distill_typed<_Float16>(a, s);
+    default: return distill_typed<__bf16>(a, s);
+  }
 }
 
 }  // namespace ifvs
