@@ -4,6 +4,15 @@
 //
 //   lookup:   out[i] = scale * sum over j of table[ids[i][j]]
 //   gradient: G[r] = scale * sum over the slots (i, j) that name r of grad[i]
+//
+// Both move bytes and add: HBM bounds them.  The gradient sorts the slots by
+// table row (stable, so equal rows stay in slot order), cuts the sorted slots
+// into equal pieces, and sums each piece's runs in order; runs that cross
+// pieces leave fp32 partial sums that a last launch adds in order.  So a row
+// that half of the slots name costs no more than as many rows, no sum depends
+// on scheduling, and each gradient row is read once.  Rows that no slot names
+// are cleared beside it.
+#include <algorithm>
 #include <cmath>
 
 #include "rows_device.h"
@@ -14,84 +23,581 @@ namespace {
 
 constexpr int kEmbThreads = 256;
 
-// One workgroup per output row.
+// Lanes that share a row: the smallest power of two that holds its vectors,
+// at most a workgroup (wider rows go to several workgroups).
+int lanes_per_row(int vecs) {
+  int l = 1;
+  while (l < vecs && l < kEmbThreads) l *= 2;
+  return l;
+}
+
+// The columns of a lane: vector `vec` of a row of dim elements.  The last
+// vector of a row that does not divide ends at the row's end: it overlaps its
+// neighbour, and only `own` of its elements (the last ones) are the lane's.
 template <typename T>
-__global__ __launch_bounds__(kEmbThreads) void embed_lookup_kernel(const EmbedArgs a) {
+struct LaneCols {
+  static constexpr int kE = Elem<T>::kPerVec;
+  int start, own;
+  bool narrow;                        // dim < kE: element by element
+  __device__ __forceinline__ LaneCols(int vec, int dim) {
+    narrow = dim < kE;
+    start = narrow ? 0 : min(vec * kE, dim - kE);
+    own = min(kE, dim - vec * kE);
+  }
+  __device__ __forceinline__ void load(const T* row, float* f) const {
+    if (!narrow) {
+      const Word4 w = *reinterpret_cast<const Word4At2*>(row + start);
+      Elem<T>::unpack(w, f);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kE; ++j) f[j] = j < own ? elem_load(row + j) : 0.0f;
+    }
+  }
+  // Elements of another type O at the same columns.
+  template <typename O>
+  __device__ __forceinline__ void load_old(const O* row, float* f) const {
+    const int skip = narrow ? 0 : kE - own;
+#pragma unroll
+    for (int j = 0; j < kE; ++j) f[j] = j >= skip && (!narrow || j < own) ? elem_load(row + start + j) : 0.0f;
+  }
+  template <typename O>
+  __device__ __forceinline__ void store(O* row, const float* f) const {
+    if (own == kE) {
+      constexpr int kO = Elem<O>::kPerVec;
+#pragma unroll
+      for (int j = 0; j < kE; j += kO) store_words(row + start + j, Elem<O>::pack(f + j));
+    } else {
+      const int skip = narrow ? 0 : kE - own;
+#pragma unroll
+      for (int j = 0; j < kE; ++j)
+        if (j >= skip && (!narrow || j < own)) row[start + j] = elem_round<O>(f[j]);
+    }
+  }
+};
+
+// grid.x: groups of kRows output rows, grid.y: kEmbThreads vectors of a row.
+template <typename T, int kRows>
+__global__ __launch_bounds__(kEmbThreads) void embed_lookup_kernel(const EmbedArgs a, int lanes, int64_t group0) {
+  constexpr int kE = Elem<T>::kPerVec;
   const T* table = static_cast<const T*>(a.table);
-  T* out = static_cast<T*>(a.out);
-  for (int64_t i = blockIdx.x; i < a.n; i += gridDim.x)
-    for (int d = threadIdx.x; d < a.dim; d += kEmbThreads) {
-      float sum = 0.0f;
-      for (int j = 0; j < a.bag; ++j) {
-        const int64_t id = a.ids[i * a.bag + j];
-        if (id >= 0 && id < a.rows) sum += elem_load(table + id * a.table_ld + d);
-      }
-      out[i * a.out_ld + d] = elem_round<T>(sum * a.scale);
+  const int lane = threadIdx.x & (lanes - 1);
+  const int groups = kEmbThreads / lanes;
+  const int64_t i0 = ((group0 + blockIdx.x) * groups + threadIdx.x / lanes) * kRows;
+  const int vec = blockIdx.y * kEmbThreads + lane;
+  if (vec * kE >= a.dim || i0 >= a.n) return;
+  const LaneCols<T> cols(vec, a.dim);
+  float sum[kRows][kE];
+#pragma unroll
+  for (int u = 0; u < kRows; ++u)
+#pragma unroll
+    for (int e = 0; e < kE; ++e) sum[u][e] = 0.0f;
+  for (int j = 0; j < a.bag; ++j) {
+    int64_t id[kRows];
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      id[u] = i0 + u < a.n ? a.ids[(i0 + u) * a.bag + j] : -1;
+      if (id[u] >= a.rows) id[u] = -1;
+    }
+    float f[kRows][kE];
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+#pragma unroll
+      for (int e = 0; e < kE; ++e) f[u][e] = 0.0f;
+      if (id[u] >= 0) cols.load(table + id[u] * a.table_ld, f[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kRows; ++u)
+#pragma unroll
+      for (int e = 0; e < kE; ++e) sum[u][e] += f[u][e];
+  }
+#pragma unroll
+  for (int u = 0; u < kRows; ++u)
+    if (i0 + u < a.n) {
+#pragma unroll
+      for (int e = 0; e < kE; ++e) sum[u][e] *= a.scale;
+      cols.store(static_cast<T*>(a.out) + (i0 + u) * a.out_ld, sum[u]);
     }
 }
 
-// One workgroup per table row: it looks through all slots in order.
-template <typename T, typename O>
-__global__ __launch_bounds__(kEmbThreads) void embed_gradient_kernel(const EmbedArgs a) {
-  __shared__ int64_t s_hit[kEmbThreads];
-  const T* grad = static_cast<const T*>(a.grad);
-  O* out = static_cast<O*>(a.out);
-  const int64_t slots = a.n * a.bag;
-  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x)
-    for (int d0 = 0; d0 < a.dim; d0 += kEmbThreads) {
-      const int d = d0 + threadIdx.x;
-      float sum = 0.0f;
-      bool any = false;
-      for (int64_t s0 = 0; s0 < slots; s0 += kEmbThreads) {
-        const int64_t s = s0 + threadIdx.x;
-        const bool hit = s < slots && a.ids[s] == r;
-        if (!__syncthreads_or(hit ? 1 : 0)) continue;
-        s_hit[threadIdx.x] = hit ? s / a.bag : -1;
-        __syncthreads();
-        for (int e = 0; e < kEmbThreads; ++e)
-          if (s_hit[e] >= 0) {
-            any = true;
-            if (d < a.dim) sum += elem_load(grad + s_hit[e] * a.grad_ld + d);
-          }
-        __syncthreads();
+// ---------------------------------------------------- sorting slots by row
+// Stable radix sort, least significant digit first.  A workgroup of 16
+// wavefronts takes tiles of 4096 entries: a wavefront ranks 64 entries at a
+// time among those of their digit (ballots over the digit's bits), so no
+// atomics order anything.
+constexpr int kSortThreads = 1024;
+constexpr int kSortWaves = kSortThreads / 64;
+constexpr int kSortRounds = 4;
+constexpr int kSortTile = kSortThreads * kSortRounds;
+constexpr int kSortMaxBits = 10;
+constexpr int kSortMaxGroups = 256;
+constexpr int64_t kSortOne = 2 * kSortTile;          // up to this one workgroup sorts alone
+
+struct SortBufs {
+  uint32_t* key;       // table row; `rows` for absent slots
+  uint32_t* from;      // gradient row
+};
+
+struct SortArgs {
+  const int32_t* ids;  // the first pass reads these
+  int64_t slots;
+  uint32_t rows;
+  int bag;
+  SortBufs in, out;
+  int shift, bits;
+  int groups;
+  int64_t per_group;   // slots of a workgroup, a multiple of kSortTile
+  uint32_t* hist;      // [groups][1 << bits]
+  uint32_t* named;     // a bit per table row
+};
+
+__device__ __forceinline__ void sort_entry(const SortArgs& a, bool first, int64_t at, uint32_t& key, uint32_t& from) {
+  if (first) {
+    const uint32_t id = static_cast<uint32_t>(a.ids[at]);
+    key = id < a.rows ? id : a.rows;
+    from = static_cast<uint32_t>(a.bag == 1 ? at : at / a.bag);
+  } else {
+    key = a.in.key[at];
+    from = a.in.from[at];
+  }
+}
+
+// Exclusive sum over 1024 threads.
+__device__ __forceinline__ uint32_t sort_scan(uint32_t v, uint32_t* s_wave) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t sum = v;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const uint32_t below = __shfl_up(sum, o, 64);
+    if (lane >= o) sum += below;
+  }
+  if (lane == 63) s_wave[wave] = sum;
+  __syncthreads();
+  uint32_t base = 0;
+  for (int w = 0; w < wave; ++w) base += s_wave[w];
+  __syncthreads();
+  return base + sum - v;
+}
+
+struct SortLds {
+  uint32_t count[kSortWaves][1 << kSortMaxBits];
+  uint32_t base[1 << kSortMaxBits];                  // where the digit's next entry goes
+  uint32_t wave[kSortWaves];
+};
+
+// Counts of the digits of [lo, hi) into s.base.
+__device__ __forceinline__ void sort_count(const SortArgs& a, bool first, int64_t lo, int64_t hi, SortLds& s) {
+  const uint32_t mask = (1u << a.bits) - 1;
+  s.base[threadIdx.x] = 0;
+  __syncthreads();
+  for (int64_t at = lo + threadIdx.x; at < hi; at += kSortThreads) {
+    uint32_t key, from;
+    sort_entry(a, first, at, key, from);
+    atomicAdd(&s.base[(key >> a.shift) & mask], 1u);
+  }
+  __syncthreads();
+}
+
+// Moves [lo, hi) to its places; s.base holds each digit's first one.
+__device__ __forceinline__ void sort_move(const SortArgs& a, bool first, int64_t lo, int64_t hi, SortLds& s) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint32_t mask = (1u << a.bits) - 1;
+  for (int64_t tile = lo; tile < hi; tile += kSortTile) {
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) s.count[w][tid] = 0;
+    __syncthreads();
+    uint32_t key[kSortRounds], from[kSortRounds], rank[kSortRounds];
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r) {
+      const int64_t at = tile + (wave * kSortRounds + r) * 64 + lane;
+      key[r] = from[r] = 0;
+      if (at < hi) sort_entry(a, first, at, key[r], from[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r) {
+      const bool live = tile + (wave * kSortRounds + r) * 64 + lane < hi;
+      const uint32_t digit = (key[r] >> a.shift) & mask;
+      uint64_t peers = __ballot(live);
+      for (int b = 0; b < a.bits; ++b) {
+        const uint64_t set = __ballot((digit >> b) & 1u);
+        peers &= (digit >> b) & 1u ? set : ~set;
       }
-      if (d < a.dim && (any || !a.accumulate)) {
-        const float old = a.accumulate ? elem_load(out + r * a.out_ld + d) : 0.0f;
-        out[r * a.out_ld + d] = elem_round<O>(old + sum * a.scale);
+      const uint32_t before = s.count[wave][digit];
+      const int below = __popcll(peers & ((1ull << lane) - 1));
+      rank[r] = before + below;
+      group_sync<64>();
+      if (live && below == 0) s.count[wave][digit] = before + __popcll(peers);
+      group_sync<64>();
+    }
+    __syncthreads();
+    // each wavefront's first place of digit `tid`
+    uint32_t next = s.base[tid];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      const uint32_t n = s.count[w][tid];
+      s.count[w][tid] = next;
+      next += n;
+    }
+    s.base[tid] = next;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r) {
+      if (tile + (wave * kSortRounds + r) * 64 + lane < hi) {
+        const uint32_t to = s.count[wave][(key[r] >> a.shift) & mask] + rank[r];
+        a.out.key[to] = key[r];
+        a.out.from[to] = from[r];
+        if (first && a.named && key[r] < a.rows) atomicOr(a.named + (key[r] >> 5), 1u << (key[r] & 31));
       }
     }
+    __syncthreads();
+  }
+}
+
+// All passes by one workgroup; passes alternate between the two buffers and
+// end in a.out (the caller orders them).
+__global__ __launch_bounds__(kSortThreads) void sort_one_kernel(SortArgs a, int passes, int64_t named_words) {
+  __shared__ SortLds s;
+  if (a.named)
+    for (int64_t w = threadIdx.x; w < named_words; w += kSortThreads) a.named[w] = 0;
+  for (int p = 0; p < passes; ++p) {
+    a.shift = p * a.bits;
+    sort_count(a, p == 0, 0, a.slots, s);
+    const uint32_t n = s.base[threadIdx.x];
+    __syncthreads();
+    const uint32_t base = sort_scan(n, s.wave);
+    s.base[threadIdx.x] = base;
+    __syncthreads();
+    sort_move(a, p == 0, 0, a.slots, s);
+    const SortBufs t = a.in;
+    a.in = a.out;
+    a.out = t;
+    __syncthreads();
+  }
+}
+
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs a, int first, int64_t named_words) {
+  __shared__ SortLds s;
+  if (first && a.named)
+    for (int64_t w = blockIdx.x * kSortThreads + threadIdx.x; w < named_words; w += gridDim.x * kSortThreads)
+      a.named[w] = 0;
+  const int64_t lo = blockIdx.x * a.per_group;
+  sort_count(a, first != 0, lo, min(a.slots, lo + a.per_group), s);
+  if (threadIdx.x < (1u << a.bits)) a.hist[(blockIdx.x << a.bits) + threadIdx.x] = s.base[threadIdx.x];
+}
+
+__global__ __launch_bounds__(kSortThreads) void sort_move_kernel(const SortArgs a, int first) {
+  __shared__ SortLds s;
+  const int tid = threadIdx.x;
+  uint32_t total = 0, before = 0;
+  if (tid < (1 << a.bits))
+    for (int g = 0; g < a.groups; ++g) {
+      const uint32_t n = a.hist[(g << a.bits) + tid];
+      if (g < static_cast<int>(blockIdx.x)) before += n;
+      total += n;
+    }
+  const uint32_t base = sort_scan(total, s.wave);
+  s.base[tid] = base + before;
+  __syncthreads();
+  const int64_t lo = blockIdx.x * a.per_group;
+  sort_move(a, first != 0, lo, min(a.slots, lo + a.per_group), s);
+}
+
+// ------------------------------------------------------------ summing runs
+constexpr int kPiece = 32;                 // sorted slots of a piece (more where pieces would pass kMaxPieces)
+constexpr int64_t kMaxPieces = 1 << 16;
+constexpr int kAhead = 8;                  // gradient rows in flight per lane
+
+struct SumArgs {
+  const uint32_t* key;       // sorted
+  const uint32_t* from;
+  int64_t slots;
+  int64_t pieces;
+  int piece;
+  float* partial;            // [pieces][2][pitch]: sums of runs that come in / go on
+  int pitch;
+  const uint32_t* named;     // null: rows without a slot stay
+  int64_t sum_blocks;        // then the clearing workgroups
+  int clear_rows;            // table rows of one
+  int lanes, col_blocks;
+};
+
+template <typename O, typename T>
+__device__ __forceinline__ void put_row(const EmbedArgs& a, const LaneCols<T>& cols, uint32_t row, const float* sum) {
+  constexpr int kE = Elem<T>::kPerVec;
+  O* out = static_cast<O*>(a.out) + static_cast<int64_t>(row) * a.out_ld;
+  float f[kE];
+  if (a.accumulate) {
+    cols.load_old(out, f);
+#pragma unroll
+    for (int e = 0; e < kE; ++e) f[e] += sum[e] * a.scale;
+  } else {
+#pragma unroll
+    for (int e = 0; e < kE; ++e) f[e] = sum[e] * a.scale;
+  }
+  cols.store(out, f);
+}
+
+template <typename O>
+__device__ __forceinline__ void clear_rows(const EmbedArgs& a, const SumArgs& s, int64_t block) {
+  constexpr int kO = Elem<O>::kPerVec;
+  const int vecs = a.dim / kO, tail = a.dim - vecs * kO;
+  const int64_t r0 = block * s.clear_rows, r1 = min(a.rows, r0 + s.clear_rows);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const Word4 zero{0, 0, 0, 0};
+  for (int64_t r = r0 + wave; r < r1; r += kEmbThreads / 64) {
+    if ((s.named[r >> 5] >> (r & 31)) & 1u) continue;
+    O* out = static_cast<O*>(a.out) + r * a.out_ld;
+    for (int v = lane; v < vecs; v += 64) store_words(out + v * kO, zero);
+    if (lane < tail) out[vecs * kO + lane] = static_cast<O>(0.0f);
+  }
+}
+
+template <typename T, typename O>
+__global__ __launch_bounds__(kEmbThreads) void embed_sum_kernel(const EmbedArgs a, const SumArgs s) {
+  constexpr int kE = Elem<T>::kPerVec;
+  const int64_t block = static_cast<int64_t>(blockIdx.x);
+  if (block >= s.sum_blocks) {
+    clear_rows<O>(a, s, block - s.sum_blocks);
+    return;
+  }
+  const int lane = threadIdx.x & (s.lanes - 1);
+  const int groups = kEmbThreads / s.lanes;
+  const int64_t piece = block / s.col_blocks * groups + threadIdx.x / s.lanes;
+  const int vec = static_cast<int>(block % s.col_blocks) * kEmbThreads + lane;
+  if (piece >= s.pieces || vec * kE >= a.dim) return;
+  const int64_t lo = piece * s.piece, hi = min(s.slots, lo + s.piece);
+  const LaneCols<T> cols(vec, a.dim);
+  const T* grad = static_cast<const T*>(a.grad);
+  float* partial = s.partial + piece * 2 * s.pitch + vec * kE;
+  const uint32_t rows = static_cast<uint32_t>(a.rows);
+  bool came_in = lo > 0 && s.key[lo - 1] == s.key[lo];
+  float sum[kE];
+#pragma unroll
+  for (int e = 0; e < kE; ++e) sum[e] = 0.0f;
+  uint32_t run = s.key[lo];
+  auto flush = [&](bool goes_on) {
+    if (run >= rows) return;
+    if (came_in || goes_on) {
+      float* to = partial + (came_in ? 0 : s.pitch);
+#pragma unroll
+      for (int e = 0; e < kE; e += 4) *reinterpret_cast<float4*>(to + e) = {sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
+    } else {
+      put_row<O>(a, cols, run, sum);
+    }
+  };
+  for (int64_t at = lo; at < hi; at += kAhead) {
+    uint32_t key[kAhead];
+    float f[kAhead][kE];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      key[u] = at + u < hi ? s.key[at + u] : rows;
+#pragma unroll
+      for (int e = 0; e < kE; ++e) f[u][e] = 0.0f;
+      if (key[u] < rows) cols.load(grad + static_cast<int64_t>(s.from[at + u]) * a.grad_ld, f[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (key[u] != run && at + u < hi) {
+        flush(false);
+        came_in = false;
+        run = key[u];
+#pragma unroll
+        for (int e = 0; e < kE; ++e) sum[e] = 0.0f;
+      }
+#pragma unroll
+      for (int e = 0; e < kE; ++e) sum[e] += f[u][e];
+    }
+  }
+  flush(hi < s.slots && s.key[hi] == run);
+}
+
+// A run that starts in a piece and goes on: its partial sums in order.
+template <typename T, typename O>
+__global__ __launch_bounds__(kEmbThreads) void embed_join_kernel(const EmbedArgs a, const SumArgs s) {
+  constexpr int kE = Elem<T>::kPerVec;
+  const int lane = threadIdx.x & (s.lanes - 1);
+  const int groups = kEmbThreads / s.lanes;
+  const int64_t piece = static_cast<int64_t>(blockIdx.x) / s.col_blocks * groups + threadIdx.x / s.lanes;
+  const int vec = static_cast<int>(blockIdx.x % s.col_blocks) * kEmbThreads + lane;
+  if (piece >= s.pieces || vec * kE >= a.dim) return;
+  const int64_t lo = piece * s.piece, hi = lo + s.piece;
+  if (hi >= s.slots) return;
+  const uint32_t run = s.key[hi - 1];
+  if (run >= static_cast<uint32_t>(a.rows) || s.key[hi] != run) return;
+  if (s.key[lo] == run && lo > 0 && s.key[lo - 1] == run) return;      // it started earlier
+  float sum[kE];
+  auto add = [&](const float* from) {
+#pragma unroll
+    for (int e = 0; e < kE; e += 4) {
+      const float4 p = *reinterpret_cast<const float4*>(from + e);
+      sum[e] += p.x;
+      sum[e + 1] += p.y;
+      sum[e + 2] += p.z;
+      sum[e + 3] += p.w;
+    }
+  };
+#pragma unroll
+  for (int e = 0; e < kE; ++e) sum[e] = 0.0f;
+  add(s.partial + (piece * 2 + 1) * s.pitch + vec * kE);
+  for (int64_t p = piece + 1; p < s.pieces && s.key[p * s.piece] == run; ++p)
+    add(s.partial + p * 2 * s.pitch + vec * kE);
+  put_row<O>(a, LaneCols<T>(vec, a.dim), run, sum);
+}
+
+// ---------------------------------------------------------------- the plan
+struct EmbedPlan {
+  int bits, passes, groups;
+  int64_t per_group, pieces;
+  int piece;
+  int64_t off_a, off_b, off_hist, off_named, off_partial, bytes, named_words;
+  int pitch;
+};
+
+int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+EmbedPlan embed_plan(int64_t rows, int dim, int64_t slots) {
+  EmbedPlan p{};
+  int bits = 1;
+  while ((rows >> bits) != 0) ++bits;                 // `rows` itself is a key
+  p.passes = (bits + kSortMaxBits - 1) / kSortMaxBits;
+  p.bits = (bits + p.passes - 1) / p.passes;
+  const int64_t tiles = (slots + kSortTile - 1) / kSortTile;
+  p.per_group = (tiles + kSortMaxGroups - 1) / kSortMaxGroups * kSortTile;
+  p.groups = static_cast<int>(slots > 0 ? (slots + p.per_group - 1) / p.per_group : 0);
+  p.piece = static_cast<int>(std::max<int64_t>(kPiece, round_up((slots + kMaxPieces - 1) / kMaxPieces, kAhead)));
+  p.pieces = (slots + p.piece - 1) / p.piece;
+  p.pitch = static_cast<int>(round_up(dim, 8));
+  p.named_words = (rows + 31) / 32;
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t off = at;
+    at += round_up(bytes, 256);
+    return off;
+  };
+  p.off_a = take(slots * 8);
+  p.off_b = take(slots * 8);
+  p.off_hist = take(static_cast<int64_t>(p.groups) * 4 << p.bits);
+  p.off_named = take(p.named_words * 4);
+  p.off_partial = take(p.pieces * 2 * p.pitch * 4);
+  p.bytes = at;
+  return p;
+}
+
+template <typename T>
+hipError_t lookup_typed(const EmbedArgs& a, hipStream_t s) {
+  const int vecs = (a.dim + Elem<T>::kPerVec - 1) / Elem<T>::kPerVec;
+  const int lanes = lanes_per_row(vecs), groups = kEmbThreads / lanes;
+  const int col_blocks = (vecs + kEmbThreads - 1) / kEmbThreads;
+  constexpr int kRows = 4;
+  // Four rows a lane keep four loads in flight; fewer rows than fill the GPU
+  // twice that way get a lane each.
+  const bool many = a.n * lanes * col_blocks >= int64_t{2} * 256 * 1024 * kRows;
+  const int per = groups * (many ? kRows : 1);
+  const int64_t blocks = (a.n + per - 1) / per;
+  constexpr int64_t kMost = 1 << 22;
+  for (int64_t at = 0; at < blocks; at += kMost) {
+    const dim3 grid(static_cast<unsigned>(std::min(blocks - at, kMost)), col_blocks);
+    if (many) embed_lookup_kernel<T, kRows><<<grid, kEmbThreads, 0, s>>>(a, lanes, at);
+    else embed_lookup_kernel<T, 1><<<grid, kEmbThreads, 0, s>>>(a, lanes, at);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t sort_slots(const EmbedArgs& a, const EmbedPlan& p, int64_t slots, char* ws, hipStream_t s, SumArgs& sum) {
+  SortArgs o{};
+  o.ids = a.ids;
+  o.slots = slots;
+  o.rows = static_cast<uint32_t>(a.rows);
+  o.bag = a.bag;
+  o.bits = p.bits;
+  o.groups = p.groups;
+  o.per_group = p.per_group;
+  o.hist = reinterpret_cast<uint32_t*>(ws + p.off_hist);
+  o.named = a.accumulate ? nullptr : reinterpret_cast<uint32_t*>(ws + p.off_named);
+  SortBufs buf[2];
+  buf[0].key = reinterpret_cast<uint32_t*>(ws + p.off_a);
+  buf[1].key = reinterpret_cast<uint32_t*>(ws + p.off_b);
+  for (SortBufs& b : buf) b.from = b.key + slots;
+  int to = 0;
+  if (slots <= kSortOne) {
+    o.out = buf[0];
+    o.in = buf[1];
+    sort_one_kernel<<<1, kSortThreads, 0, s>>>(o, p.passes, o.named ? p.named_words : 0);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    to = (p.passes - 1) & 1;
+  } else {
+    for (int pass = 0; pass < p.passes; ++pass) {
+      to = pass & 1;
+      o.shift = pass * p.bits;
+      o.in = buf[to ^ 1];
+      o.out = buf[to];
+      sort_count_kernel<<<p.groups, kSortThreads, 0, s>>>(o, pass == 0, p.named_words);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+      sort_move_kernel<<<p.groups, kSortThreads, 0, s>>>(o, pass == 0);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+  }
+  sum.key = buf[to].key;
+  sum.from = buf[to].from;
+  sum.named = o.named;
+  return hipSuccess;
+}
+
+template <typename T, typename O>
+hipError_t gradient_typed(const EmbedArgs& a, hipStream_t s) {
+  const int64_t slots = a.n * a.bag;
+  const EmbedPlan p = embed_plan(a.rows, a.dim, slots);
+  char* ws = static_cast<char*>(a.workspace);
+  SumArgs sum{};
+  if (slots > 0) {
+    if (hipError_t e = sort_slots(a, p, slots, ws, s, sum); e != hipSuccess) return e;
+  } else {
+    sum.named = reinterpret_cast<uint32_t*>(ws + p.off_named);
+    SortArgs o{};
+    o.named = const_cast<uint32_t*>(sum.named);
+    sort_one_kernel<<<1, kSortThreads, 0, s>>>(o, 0, p.named_words);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  const int vecs = (a.dim + Elem<T>::kPerVec - 1) / Elem<T>::kPerVec;
+  sum.slots = slots;
+  sum.piece = p.piece;
+  sum.pieces = p.pieces;
+  sum.partial = reinterpret_cast<float*>(ws + p.off_partial);
+  sum.pitch = p.pitch;
+  sum.lanes = lanes_per_row(vecs);
+  sum.col_blocks = (vecs + kEmbThreads - 1) / kEmbThreads;
+  const int groups = kEmbThreads / sum.lanes;
+  sum.sum_blocks = (p.pieces + groups - 1) / groups * sum.col_blocks;
+  // A clearing workgroup takes about 64 KB of table.
+  const int64_t row_bytes = static_cast<int64_t>(a.dim) * sizeof(O);
+  sum.clear_rows = static_cast<int>(std::clamp<int64_t>(65536 / row_bytes, 4, 4096));
+  const int64_t clear = sum.named ? (a.rows + sum.clear_rows - 1) / sum.clear_rows : 0;
+  embed_sum_kernel<T, O><<<static_cast<unsigned>(sum.sum_blocks + clear), kEmbThreads, 0, s>>>(a, sum);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || p.pieces <= 1) return e;
+  embed_join_kernel<T, O><<<static_cast<unsigned>(sum.sum_blocks), kEmbThreads, 0, s>>>(a, sum);
+  return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t embed_workspace_bytes(int64_t, int, int64_t) { return 0; }
+int64_t embed_workspace_bytes(int64_t rows, int dim, int64_t slots) { return embed_plan(rows, dim, slots).bytes; }
 
 hipError_t launch_embed_lookup(const EmbedArgs& a, hipStream_t s) {
   if (a.n == 0) return hipSuccess;
-  const dim3 grid(static_cast<unsigned>(a.n < 65536 ? a.n : 65536)), block(kEmbThreads);
   switch (a.dtype) {
-    case kElemF32: embed_lookup_kernel<float><<<grid, block, 0, s>>>(a); break;
-    case kElemF16: embed_lookup_kernel<_Float16><<<grid, block, 0, s>>>(a); break;
-    default: embed_lookup_kernel<__bf16><<<grid, block, 0, s>>>(a); break;
+    case kElemF32: return lookup_typed<float>(a, s);
+    case kElemF16: return lookup_typed<_Float16>(a, s);
+    default: return lookup_typed<__bf16>(a, s);
   }
-  return hipGetLastError();
 }
 
 hipError_t launch_embed_gradient(const EmbedArgs& a, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(a.rows < 65536 ? a.rows : 65536)), block(kEmbThreads);
   const bool wide = a.out_dtype == kElemF32;
   switch (a.dtype) {
-    case kElemF32: embed_gradient_kernel<float, float><<<grid, block, 0, s>>>(a); break;
-    case kElemF16:
-      if (wide) embed_gradient_kernel<_Float16, float><<<grid, block, 0, s>>>(a);
-      else embed_gradient_kernel<_Float16, _Float16><<<grid, block, 0, s>>>(a);
-      break;
-    default:
-      if (wide) embed_gradient_kernel<__bf16, float><<<grid, block, 0, s>>>(a);
-      else embed_gradient_kernel<__bf16, __bf16><<<grid, block, 0, s>>>(a);
-      break;
+    case kElemF32: return gradient_typed<float, float>(a, s);
+    case kElemF16: return wide ? gradient_typed<_Float16, float>(a, s) : gradient_typed<_Float16, _Float16>(a, s);
+    default: return wide ? gradient_typed<__bf16, float>(a, s) : gradient_typed<__bf16, __bf16>(a, s);
   }
-  return hipGetLastError();
 }
 
 }  // namespace ifvs
