@@ -44,14 +44,13 @@ struct LaneCols {
     start = narrow ? 0 : min(vec * kE, dim - kE);
     own = min(kE, dim - vec * kE);
   }
-  __device__ __forceinline__ void load(const T* row, float* f) const {
-    if (!narrow) {
-      const Word4 w = *reinterpret_cast<const Word4At2*>(row + start);
-      Elem<T>::unpack(w, f);
-    } else {
+  // The lane's vector of a row, packed.
+  __device__ __forceinline__ Word4 load_raw(const T* row) const {
+    if (!narrow) return *reinterpret_cast<const Word4At2*>(row + start);
+    float f[kE];
 #pragma unroll
-      for (int j = 0; j < kE; ++j) f[j] = j < own ? elem_load(row + j) : 0.0f;
-    }
+    for (int j = 0; j < kE; ++j) f[j] = j < own ? elem_load(row + j) : 0.0f;
+    return Elem<T>::pack(f);
   }
   // Elements of another type O at the same columns.
   template <typename O>
@@ -92,23 +91,22 @@ __global__ __launch_bounds__(kEmbThreads) void embed_lookup_kernel(const EmbedAr
 #pragma unroll
     for (int e = 0; e < kE; ++e) sum[u][e] = 0.0f;
   for (int j = 0; j < a.bag; ++j) {
-    int64_t id[kRows];
+    // Absent slots and rows past the end read row 0 and drop it: no load
+    // waits for a branch.
+    uint32_t id[kRows];
+    Word4 w[kRows];
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-      id[u] = i0 + u < a.n ? a.ids[(i0 + u) * a.bag + j] : -1;
-      if (id[u] >= a.rows) id[u] = -1;
-    }
-    float f[kRows][kE];
-#pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-#pragma unroll
-      for (int e = 0; e < kE; ++e) f[u][e] = 0.0f;
-      if (id[u] >= 0) cols.load(table + id[u] * a.table_ld, f[u]);
-    }
+    for (int u = 0; u < kRows; ++u) id[u] = static_cast<uint32_t>(a.ids[min(i0 + u, a.n - 1) * a.bag + j]);
 #pragma unroll
     for (int u = 0; u < kRows; ++u)
+      w[u] = cols.load_raw(table + (id[u] < static_cast<uint32_t>(a.rows) ? static_cast<int64_t>(id[u]) : 0) * a.table_ld);
 #pragma unroll
-      for (int e = 0; e < kE; ++e) sum[u][e] += f[u][e];
+    for (int u = 0; u < kRows; ++u) {
+      float f[kE];
+      Elem<T>::unpack(w[u], f);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) sum[u][e] += id[u] < static_cast<uint32_t>(a.rows) ? f[e] : 0.0f;
+    }
   }
 #pragma unroll
   for (int u = 0; u < kRows; ++u)
@@ -288,11 +286,17 @@ __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(const SortArgs 
   __shared__ SortLds s;
   const int tid = threadIdx.x;
   uint32_t total = 0, before = 0;
+  constexpr int kAtOnce = 8;
   if (tid < (1 << a.bits))
-    for (int g = 0; g < a.groups; ++g) {
-      const uint32_t n = a.hist[(g << a.bits) + tid];
-      if (g < static_cast<int>(blockIdx.x)) before += n;
-      total += n;
+    for (int g = 0; g < a.groups; g += kAtOnce) {
+      uint32_t n[kAtOnce];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) n[u] = g + u < a.groups ? a.hist[((g + u) << a.bits) + tid] : 0;
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        if (g + u < static_cast<int>(blockIdx.x)) before += n[u];
+        total += n[u];
+      }
     }
   const uint32_t base = sort_scan(total, s.wave);
   s.base[tid] = base + before;
@@ -303,7 +307,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(const SortArgs 
 
 // ------------------------------------------------------------ summing runs
 constexpr int kPiece = 32;                 // sorted slots of a piece (more where pieces would pass kMaxPieces)
-constexpr int64_t kMaxPieces = 1 << 16;
+constexpr int64_t kMaxPieces = 1 << 13;
 constexpr int kAhead = 8;                  // gradient rows in flight per lane
 
 struct SumArgs {
@@ -385,15 +389,17 @@ __global__ __launch_bounds__(kEmbThreads) void embed_sum_kernel(const EmbedArgs 
     }
   };
   for (int64_t at = lo; at < hi; at += kAhead) {
-    uint32_t key[kAhead];
-    float f[kAhead][kE];
+    // Absent slots' rows are read too (their run is dropped), and past the
+    // end the last slot's again: no load waits for a branch.
+    uint32_t key[kAhead], from[kAhead];
+    Word4 w[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      key[u] = at + u < hi ? s.key[at + u] : rows;
-#pragma unroll
-      for (int e = 0; e < kE; ++e) f[u][e] = 0.0f;
-      if (key[u] < rows) cols.load(grad + static_cast<int64_t>(s.from[at + u]) * a.grad_ld, f[u]);
+      key[u] = s.key[min(at + u, hi - 1)];
+      from[u] = s.from[min(at + u, hi - 1)];
     }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) w[u] = cols.load_raw(grad + static_cast<int64_t>(from[u]) * a.grad_ld);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       if (key[u] != run && at + u < hi) {
@@ -403,8 +409,12 @@ __global__ __launch_bounds__(kEmbThreads) void embed_sum_kernel(const EmbedArgs 
 #pragma unroll
         for (int e = 0; e < kE; ++e) sum[e] = 0.0f;
       }
+      if (at + u < hi) {
+        float f[kE];
+        Elem<T>::unpack(w[u], f);
 #pragma unroll
-      for (int e = 0; e < kE; ++e) sum[e] += f[u][e];
+        for (int e = 0; e < kE; ++e) sum[e] += f[e];
+      }
     }
   }
   flush(hi < s.slots && s.key[hi] == run);
@@ -424,22 +434,46 @@ __global__ __launch_bounds__(kEmbThreads) void embed_join_kernel(const EmbedArgs
   const uint32_t run = s.key[hi - 1];
   if (run >= static_cast<uint32_t>(a.rows) || s.key[hi] != run) return;
   if (s.key[lo] == run && lo > 0 && s.key[lo - 1] == run) return;      // it started earlier
+  // Partial sums in order, kJoinAhead in flight; the keys that say whether the
+  // next ones belong to the run are read one step ahead of them.
+  constexpr uint32_t kJoinAhead = 16;
   float sum[kE];
-  auto add = [&](const float* from) {
+  {
+    const float* from = s.partial + (piece * 2 + 1) * s.pitch + vec * kE;
 #pragma unroll
-    for (int e = 0; e < kE; e += 4) {
-      const float4 p = *reinterpret_cast<const float4*>(from + e);
-      sum[e] += p.x;
-      sum[e + 1] += p.y;
-      sum[e + 2] += p.z;
-      sum[e + 3] += p.w;
-    }
+    for (int e = 0; e < kE; ++e) sum[e] = from[e];
+  }
+  // (No load waits for another: past the end both read the last piece's.)
+  auto look = [&](int64_t p0) {
+    uint32_t key[kJoinAhead], m = 0;
+#pragma unroll
+    for (uint32_t u = 0; u < kJoinAhead; ++u) key[u] = s.key[min(p0 + u, s.pieces - 1) * s.piece];
+#pragma unroll
+    for (uint32_t u = 0; u < kJoinAhead; ++u) m += key[u] == run && p0 + u < s.pieces ? 1 : 0;
+    return m;
   };
+  uint32_t mine = look(piece + 1);
+  for (int64_t p0 = piece + 1; mine != 0; p0 += kJoinAhead) {
+    float4 f[kJoinAhead][kE / 4];
 #pragma unroll
-  for (int e = 0; e < kE; ++e) sum[e] = 0.0f;
-  add(s.partial + (piece * 2 + 1) * s.pitch + vec * kE);
-  for (int64_t p = piece + 1; p < s.pieces && s.key[p * s.piece] == run; ++p)
-    add(s.partial + p * 2 * s.pitch + vec * kE);
+    for (uint32_t u = 0; u < kJoinAhead; ++u)
+#pragma unroll
+      for (int e = 0; e < kE / 4; ++e)
+        f[u][e] = *reinterpret_cast<const float4*>(s.partial + min(p0 + u, s.pieces - 1) * 2 * s.pitch + vec * kE + 4 * e);
+    const uint32_t now = mine;
+    mine = now == kJoinAhead ? look(p0 + kJoinAhead) : 0;
+#pragma unroll
+    for (uint32_t u = 0; u < kJoinAhead; ++u)
+      if (u < now) {
+#pragma unroll
+        for (int e = 0; e < kE / 4; ++e) {
+          sum[4 * e] += f[u][e].x;
+          sum[4 * e + 1] += f[u][e].y;
+          sum[4 * e + 2] += f[u][e].z;
+          sum[4 * e + 3] += f[u][e].w;
+        }
+      }
+  }
   put_row<O>(a, LaneCols<T>(vec, a.dim), run, sum);
 }
 
