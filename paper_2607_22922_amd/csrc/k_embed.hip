@@ -128,7 +128,11 @@ constexpr int kSortRounds = 4;
 constexpr int kSortTile = kSortThreads * kSortRounds;
 constexpr int kSortMaxBits = 10;
 constexpr int kSortMaxGroups = 256;
-constexpr int64_t kSortOne = 2 * kSortTile;          // up to this one workgroup sorts alone
+// One launch (sort_owned_kernel) up to this many slots and owners: each owner
+// reads all ids twice, so its time grows with slots x owners.
+constexpr int64_t kOwnedSlots = 1 << 17;
+constexpr int kOwnersFull = 256;
+constexpr int64_t kMostOwners = 1 << 9;
 
 struct SortBufs {
   uint32_t* key;       // table row; `rows` for absent slots
@@ -152,7 +156,7 @@ __device__ __forceinline__ void sort_entry(const SortArgs& a, bool first, int64_
   if (first) {
     const uint32_t id = static_cast<uint32_t>(a.ids[at]);
     key = id < a.rows ? id : a.rows;
-    from = static_cast<uint32_t>(a.bag == 1 ? at : at / a.bag);
+    from = a.bag == 1 ? static_cast<uint32_t>(at) : static_cast<uint32_t>(at) / static_cast<uint32_t>(a.bag);
   } else {
     key = a.in.key[at];
     from = a.in.from[at];
@@ -200,8 +204,9 @@ __device__ __forceinline__ void sort_move(const SortArgs& a, bool first, int64_t
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const uint32_t mask = (1u << a.bits) - 1;
   for (int64_t tile = lo; tile < hi; tile += kSortTile) {
+    if (tid <= static_cast<int>(mask))
 #pragma unroll
-    for (int w = 0; w < kSortWaves; ++w) s.count[w][tid] = 0;
+      for (int w = 0; w < kSortWaves; ++w) s.count[w][tid] = 0;
     __syncthreads();
     uint32_t key[kSortRounds], from[kSortRounds], rank[kSortRounds];
 #pragma unroll
@@ -228,14 +233,16 @@ __device__ __forceinline__ void sort_move(const SortArgs& a, bool first, int64_t
     }
     __syncthreads();
     // each wavefront's first place of digit `tid`
-    uint32_t next = s.base[tid];
+    if (tid <= static_cast<int>(mask)) {
+      uint32_t next = s.base[tid];
 #pragma unroll
-    for (int w = 0; w < kSortWaves; ++w) {
-      const uint32_t n = s.count[w][tid];
-      s.count[w][tid] = next;
-      next += n;
+      for (int w = 0; w < kSortWaves; ++w) {
+        const uint32_t n = s.count[w][tid];
+        s.count[w][tid] = next;
+        next += n;
+      }
+      s.base[tid] = next;
     }
-    s.base[tid] = next;
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kSortRounds; ++r) {
@@ -250,26 +257,83 @@ __device__ __forceinline__ void sort_move(const SortArgs& a, bool first, int64_t
   }
 }
 
-// All passes by one workgroup; passes alternate between the two buffers and
-// end in a.out (the caller orders them).
-__global__ __launch_bounds__(kSortThreads) void sort_one_kernel(SortArgs a, int passes, int64_t named_words) {
+// Few slots, in one launch: every workgroup owns 1 << bits table rows, looks
+// through all ids for them (the L2 holds the ids), moves its slots, in order,
+// to where they lie in the whole order (it has counted the smaller ids on the
+// way), and sorts them there by one pass.  The owner of the last rows takes
+// the absent slots.
+__global__ __launch_bounds__(kSortThreads) void sort_owned_kernel(SortArgs a) {
   __shared__ SortLds s;
-  if (a.named)
-    for (int64_t w = threadIdx.x; w < named_words; w += kSortThreads) a.named[w] = 0;
-  for (int p = 0; p < passes; ++p) {
-    a.shift = p * a.bits;
-    sort_count(a, p == 0, 0, a.slots, s);
-    const uint32_t n = s.base[threadIdx.x];
-    __syncthreads();
-    const uint32_t base = sort_scan(n, s.wave);
-    s.base[threadIdx.x] = base;
-    __syncthreads();
-    sort_move(a, p == 0, 0, a.slots, s);
-    const SortBufs t = a.in;
-    a.in = a.out;
-    a.out = t;
-    __syncthreads();
+  __shared__ uint32_t s_below[kSortWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint32_t first = blockIdx.x << a.bits, last = first + (1u << a.bits);
+  // a wavefront's slots, 64 a round; kHeld rounds stay in registers, so up to
+  // 32768 slots are read once and with one wait
+  const int64_t per_wave = (a.slots + kSortThreads - 1) / kSortThreads * 64;
+  const int64_t lo = wave * per_wave, hi = min(a.slots, lo + per_wave);
+  constexpr int kHeld = 32;
+  uint32_t key[kHeld];
+  bool held = false;
+  auto each = [&](auto&& fn) {
+    for (int64_t at = lo; at < hi; at += 64 * kHeld) {
+      if (!held) {
+#pragma unroll
+        for (int u = 0; u < kHeld; ++u) {
+          key[u] = 0;
+          if (at + u * 64 < hi) key[u] = min(static_cast<uint32_t>(a.ids[min(at + u * 64 + lane, a.slots - 1)]), a.rows);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kHeld; ++u) {
+        const int64_t mine = at + u * 64 + lane;
+        if (at + u * 64 < hi) fn(mine, mine < hi, key[u]);
+      }
+    }
+    held = per_wave <= 64 * kHeld;
+  };
+  uint32_t below = 0, own = 0;
+  each([&](int64_t, bool live, uint32_t key) {
+    below += __popcll(__ballot(live && key < first));
+    own += __popcll(__ballot(live && key >= first && key < last));
+  });
+  if (lane == 0) {
+    s_below[wave] = below;
+    s.wave[wave] = own;
   }
+  __syncthreads();
+  uint32_t start = 0, to = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) {
+    start += s_below[w];
+    if (w < wave) to += s.wave[w];
+    total += s.wave[w];
+  }
+  to += start;
+  if (own > 0)
+    each([&](int64_t at, bool live, uint32_t key) {
+      const bool mine = live && key >= first && key < last;
+      const uint64_t hits = __ballot(mine);
+      if (mine) {
+        const uint32_t p = to + __popcll(hits & ((1ull << lane) - 1));
+        a.in.key[p] = key;
+        a.in.from[p] = a.bag == 1 ? static_cast<uint32_t>(at) : static_cast<uint32_t>(at) / static_cast<uint32_t>(a.bag);
+      }
+      to += __popcll(hits);
+    });
+  __syncthreads();
+  sort_count(a, false, start, start + total, s);
+  const uint32_t n = s.base[tid];
+  if (a.named && tid < (1 << a.bits)) {               // bits >= 6: whole words
+    const uint64_t set = __ballot(n > 0 && first + tid < a.rows);
+    const uint32_t word = (first + tid) >> 5;
+    if (lane % 32 == 0 && first + tid < a.rows) a.named[word] = static_cast<uint32_t>(set >> lane);
+  }
+  if (total == 0) return;
+  __syncthreads();
+  const uint32_t base = sort_scan(n, s.wave);
+  s.base[tid] = start + base;
+  __syncthreads();
+  sort_move(a, false, start, start + total, s);
 }
 
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs a, int first, int64_t named_words) {
@@ -306,7 +370,12 @@ __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(const SortArgs 
 }
 
 // ------------------------------------------------------------ summing runs
-constexpr int kPiece = 32;                 // sorted slots of a piece (more where pieces would pass kMaxPieces)
+// Sorted slots of a piece: few slots need many pieces to fill the GPU, many
+// slots fewer partial sums (32768 slots, a row of 13% of them: joining 19 -> 11
+// us); kMaxPieces bounds the longest join.
+constexpr int kPiece = 32;
+constexpr int kLongPiece = 64;
+constexpr int64_t kLongSlots = 1 << 14;
 constexpr int64_t kMaxPieces = 1 << 13;
 constexpr int kAhead = 8;                  // gradient rows in flight per lane
 
@@ -318,7 +387,7 @@ struct SumArgs {
   int piece;
   float* partial;            // [pieces][2][pitch]: sums of runs that come in / go on
   int pitch;
-  const uint32_t* named;     // null: rows without a slot stay
+  const uint32_t* named;     // null: no slot at all
   int64_t sum_blocks;        // then the clearing workgroups
   int clear_rows;            // table rows of one
   int lanes, col_blocks;
@@ -348,7 +417,7 @@ __device__ __forceinline__ void clear_rows(const EmbedArgs& a, const SumArgs& s,
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const Word4 zero{0, 0, 0, 0};
   for (int64_t r = r0 + wave; r < r1; r += kEmbThreads / 64) {
-    if ((s.named[r >> 5] >> (r & 31)) & 1u) continue;
+    if (s.named && ((s.named[r >> 5] >> (r & 31)) & 1u)) continue;
     O* out = static_cast<O*>(a.out) + r * a.out_ld;
     for (int v = lane; v < vecs; v += 64) store_words(out + v * kO, zero);
     if (lane < tail) out[vecs * kO + lane] = static_cast<O>(0.0f);
@@ -420,14 +489,18 @@ __global__ __launch_bounds__(kEmbThreads) void embed_sum_kernel(const EmbedArgs 
   flush(hi < s.slots && s.key[hi] == run);
 }
 
-// A run that starts in a piece and goes on: its partial sums in order.
+// A run that starts in a piece and goes on: its partial sums in order.  One
+// CU reads some 40 GB/s: a long run's columns go to workgroups of a wavefront
+// (2048 columns, 137 pieces: 26 -> 9 us).
+constexpr int kJoinThreads = 64;
 template <typename T, typename O>
-__global__ __launch_bounds__(kEmbThreads) void embed_join_kernel(const EmbedArgs a, const SumArgs s) {
+__global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(const EmbedArgs a, const SumArgs s, int lanes,
+                                                                  int col_blocks) {
   constexpr int kE = Elem<T>::kPerVec;
-  const int lane = threadIdx.x & (s.lanes - 1);
-  const int groups = kEmbThreads / s.lanes;
-  const int64_t piece = static_cast<int64_t>(blockIdx.x) / s.col_blocks * groups + threadIdx.x / s.lanes;
-  const int vec = static_cast<int>(blockIdx.x % s.col_blocks) * kEmbThreads + lane;
+  const int lane = threadIdx.x & (lanes - 1);
+  const int groups = kJoinThreads / lanes;
+  const int64_t piece = static_cast<int64_t>(blockIdx.x) / col_blocks * groups + threadIdx.x / lanes;
+  const int vec = static_cast<int>(blockIdx.x % col_blocks) * kJoinThreads + lane;
   if (piece >= s.pieces || vec * kE >= a.dim) return;
   const int64_t lo = piece * s.piece, hi = lo + s.piece;
   if (hi >= s.slots) return;
@@ -479,7 +552,7 @@ __global__ __launch_bounds__(kEmbThreads) void embed_join_kernel(const EmbedArgs
 
 // ---------------------------------------------------------------- the plan
 struct EmbedPlan {
-  int bits, passes, groups;
+  int bits, passes, groups;          // passes 0: sort_owned_kernel, groups owners
   int64_t per_group, pieces;
   int piece;
   int64_t off_a, off_b, off_hist, off_named, off_partial, bytes, named_words;
@@ -492,12 +565,19 @@ EmbedPlan embed_plan(int64_t rows, int dim, int64_t slots) {
   EmbedPlan p{};
   int bits = 1;
   while ((rows >> bits) != 0) ++bits;                 // `rows` itself is a key
-  p.passes = (bits + kSortMaxBits - 1) / kSortMaxBits;
-  p.bits = (bits + p.passes - 1) / p.passes;
-  const int64_t tiles = (slots + kSortTile - 1) / kSortTile;
-  p.per_group = (tiles + kSortMaxGroups - 1) / kSortMaxGroups * kSortTile;
-  p.groups = static_cast<int>(slots > 0 ? (slots + p.per_group - 1) / p.per_group : 0);
-  p.piece = static_cast<int>(std::max<int64_t>(kPiece, round_up((slots + kMaxPieces - 1) / kMaxPieces, kAhead)));
+  int own = 6;                                        // a wavefront writes whole words of the named bits
+  while (own < kSortMaxBits && (rows >> own) >= kOwnersFull) ++own;
+  if (slots <= kOwnedSlots && (rows >> own) < kMostOwners) {
+    p.bits = own;
+    p.groups = static_cast<int>((rows >> own) + 1);
+  } else {
+    p.passes = (bits + kSortMaxBits - 1) / kSortMaxBits;
+    p.bits = (bits + p.passes - 1) / p.passes;
+    const int64_t tiles = (slots + kSortTile - 1) / kSortTile;
+    p.per_group = (tiles + kSortMaxGroups - 1) / kSortMaxGroups * kSortTile;
+    p.groups = static_cast<int>((slots + p.per_group - 1) / p.per_group);
+  }
+  p.piece = static_cast<int>(std::max<int64_t>(slots < kLongSlots ? kPiece : kLongPiece, round_up((slots + kMaxPieces - 1) / kMaxPieces, kAhead)));
   p.pieces = (slots + p.piece - 1) / p.piece;
   p.pitch = static_cast<int>(round_up(dim, 8));
   p.named_words = (rows + 31) / 32;
@@ -509,7 +589,7 @@ EmbedPlan embed_plan(int64_t rows, int dim, int64_t slots) {
   };
   p.off_a = take(slots * 8);
   p.off_b = take(slots * 8);
-  p.off_hist = take(static_cast<int64_t>(p.groups) * 4 << p.bits);
+  p.off_hist = take(p.passes > 0 ? static_cast<int64_t>(p.groups) * 4 << p.bits : 0);
   p.off_named = take(p.named_words * 4);
   p.off_partial = take(p.pieces * 2 * p.pitch * 4);
   p.bytes = at;
@@ -553,12 +633,11 @@ hipError_t sort_slots(const EmbedArgs& a, const EmbedPlan& p, int64_t slots, cha
   buf[1].key = reinterpret_cast<uint32_t*>(ws + p.off_b);
   for (SortBufs& b : buf) b.from = b.key + slots;
   int to = 0;
-  if (slots <= kSortOne) {
-    o.out = buf[0];
+  if (p.passes == 0) {
     o.in = buf[1];
-    sort_one_kernel<<<1, kSortThreads, 0, s>>>(o, p.passes, o.named ? p.named_words : 0);
+    o.out = buf[0];
+    sort_owned_kernel<<<p.groups, kSortThreads, 0, s>>>(o);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    to = (p.passes - 1) & 1;
   } else {
     for (int pass = 0; pass < p.passes; ++pass) {
       to = pass & 1;
@@ -583,15 +662,8 @@ hipError_t gradient_typed(const EmbedArgs& a, hipStream_t s) {
   const EmbedPlan p = embed_plan(a.rows, a.dim, slots);
   char* ws = static_cast<char*>(a.workspace);
   SumArgs sum{};
-  if (slots > 0) {
+  if (slots > 0)
     if (hipError_t e = sort_slots(a, p, slots, ws, s, sum); e != hipSuccess) return e;
-  } else {
-    sum.named = reinterpret_cast<uint32_t*>(ws + p.off_named);
-    SortArgs o{};
-    o.named = const_cast<uint32_t*>(sum.named);
-    sort_one_kernel<<<1, kSortThreads, 0, s>>>(o, 0, p.named_words);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  }
   const int vecs = (a.dim + Elem<T>::kPerVec - 1) / Elem<T>::kPerVec;
   sum.slots = slots;
   sum.piece = p.piece;
@@ -602,13 +674,17 @@ hipError_t gradient_typed(const EmbedArgs& a, hipStream_t s) {
   sum.col_blocks = (vecs + kEmbThreads - 1) / kEmbThreads;
   const int groups = kEmbThreads / sum.lanes;
   sum.sum_blocks = (p.pieces + groups - 1) / groups * sum.col_blocks;
-  // A clearing workgroup takes about 64 KB of table.
+  // A clearing workgroup takes about 64 KB of table, less where that would
+  // leave CUs idle.
   const int64_t row_bytes = static_cast<int64_t>(a.dim) * sizeof(O);
-  sum.clear_rows = static_cast<int>(std::clamp<int64_t>(65536 / row_bytes, 4, 4096));
-  const int64_t clear = sum.named ? (a.rows + sum.clear_rows - 1) / sum.clear_rows : 0;
+  sum.clear_rows = static_cast<int>(std::clamp<int64_t>(std::min(65536 / row_bytes, a.rows / 1024), 4, 4096));
+  const int64_t clear = a.accumulate ? 0 : (a.rows + sum.clear_rows - 1) / sum.clear_rows;
   embed_sum_kernel<T, O><<<static_cast<unsigned>(sum.sum_blocks + clear), kEmbThreads, 0, s>>>(a, sum);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || p.pieces <= 1) return e;
-  embed_join_kernel<T, O><<<static_cast<unsigned>(sum.sum_blocks), kEmbThreads, 0, s>>>(a, sum);
+  const int lanes = std::min(sum.lanes, kJoinThreads), per = kJoinThreads / lanes;
+  const int col_blocks = (vecs + kJoinThreads - 1) / kJoinThreads;
+  embed_join_kernel<T, O><<<static_cast<unsigned>((p.pieces + per - 1) / per * col_blocks), kJoinThreads, 0, s>>>(
+      a, sum, lanes, col_blocks);
   return hipGetLastError();
 }
 
