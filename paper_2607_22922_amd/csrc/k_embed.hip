@@ -10,8 +10,8 @@
 // into equal pieces, and sums each piece's runs in order; runs that cross
 // pieces leave fp32 partial sums that a last launch adds in order.  So a row
 // that half of the slots name costs no more than as many rows, no sum depends
-// on scheduling, and each gradient row is read once.  Rows that no slot names
-// are cleared beside it.
+// on scheduling, and each gradient row is read once.  The table is cleared
+// beside the sort.
 #include <algorithm>
 #include <cmath>
 
@@ -149,7 +149,6 @@ struct SortArgs {
   int groups;
   int64_t per_group;   // slots of a workgroup, a multiple of kSortTile
   uint32_t* hist;      // [groups][1 << bits]
-  uint32_t* named;     // a bit per table row
 };
 
 __device__ __forceinline__ void sort_entry(const SortArgs& a, bool first, int64_t at, uint32_t& key, uint32_t& from) {
@@ -250,28 +249,55 @@ __device__ __forceinline__ void sort_move(const SortArgs& a, bool first, int64_t
         const uint32_t to = s.count[wave][(key[r] >> a.shift) & mask] + rank[r];
         a.out.key[to] = key[r];
         a.out.from[to] = from[r];
-        if (first && a.named && key[r] < a.rows) atomicOr(a.named + (key[r] >> 5), 1u << (key[r] & 31));
       }
     }
     __syncthreads();
   }
 }
 
+// Clears the table beside the sort (whose few workgroups wait for memory most
+// of the time): rows that slots name are written again later, which costs less
+// than to wait for the sort's answer which those are.
+struct ClearArgs {
+  char* out;
+  int64_t rows, row_bytes, stride, last_bytes;   // rows of row_bytes, the last one of last_bytes
+  int threads;                                    // of a row: a workgroup or a wavefront
+  int64_t blocks;
+};
+
+__device__ __forceinline__ void clear_rows(const ClearArgs& c, int64_t block) {
+  const Word4 zero{0, 0, 0, 0};
+  const int per = kSortThreads / c.threads, lane = threadIdx.x & (c.threads - 1);
+  for (int64_t r = block * per + threadIdx.x / c.threads; r < c.rows; r += c.blocks * per) {
+    char* out = c.out + r * c.stride;
+    const int64_t bytes = r == c.rows - 1 ? c.last_bytes : c.row_bytes;
+    const int64_t vecs = bytes >> 4;
+    for (int64_t v = lane; v < vecs; v += c.threads) store_words(out + (v << 4), zero);
+    for (int64_t h = (vecs << 3) + lane; h < bytes >> 1; h += c.threads) reinterpret_cast<uint16_t*>(out)[h] = 0;
+  }
+}
+
+__global__ __launch_bounds__(kSortThreads) void clear_kernel(const ClearArgs c) { clear_rows(c, blockIdx.x); }
+
 // Few slots, in one launch: every workgroup owns 1 << bits table rows, looks
 // through all ids for them (the L2 holds the ids), moves its slots, in order,
 // to where they lie in the whole order (it has counted the smaller ids on the
 // way), and sorts them there by one pass.  The owner of the last rows takes
 // the absent slots.
-__global__ __launch_bounds__(kSortThreads) void sort_owned_kernel(SortArgs a) {
+__global__ __launch_bounds__(kSortThreads) void sort_owned_kernel(const SortArgs a, const ClearArgs c) {
   __shared__ SortLds s;
   __shared__ uint32_t s_below[kSortWaves];
+  if (static_cast<int>(blockIdx.x) >= a.groups) {
+    clear_rows(c, blockIdx.x - a.groups);
+    return;
+  }
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const uint32_t first = blockIdx.x << a.bits, last = first + (1u << a.bits);
   // a wavefront's slots, 64 a round; kHeld rounds stay in registers, so up to
-  // 32768 slots are read once and with one wait
+  // 16384 slots are read once and with one wait
   const int64_t per_wave = (a.slots + kSortThreads - 1) / kSortThreads * 64;
   const int64_t lo = wave * per_wave, hi = min(a.slots, lo + per_wave);
-  constexpr int kHeld = 32;
+  constexpr int kHeld = 16;
   uint32_t key[kHeld];
   bool held = false;
   auto each = [&](auto&& fn) {
@@ -323,11 +349,6 @@ __global__ __launch_bounds__(kSortThreads) void sort_owned_kernel(SortArgs a) {
   __syncthreads();
   sort_count(a, false, start, start + total, s);
   const uint32_t n = s.base[tid];
-  if (a.named && tid < (1 << a.bits)) {               // bits >= 6: whole words
-    const uint64_t set = __ballot(n > 0 && first + tid < a.rows);
-    const uint32_t word = (first + tid) >> 5;
-    if (lane % 32 == 0 && first + tid < a.rows) a.named[word] = static_cast<uint32_t>(set >> lane);
-  }
   if (total == 0) return;
   __syncthreads();
   const uint32_t base = sort_scan(n, s.wave);
@@ -336,11 +357,12 @@ __global__ __launch_bounds__(kSortThreads) void sort_owned_kernel(SortArgs a) {
   sort_move(a, false, start, start + total, s);
 }
 
-__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs a, int first, int64_t named_words) {
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs a, int first, const ClearArgs c) {
   __shared__ SortLds s;
-  if (first && a.named)
-    for (int64_t w = blockIdx.x * kSortThreads + threadIdx.x; w < named_words; w += gridDim.x * kSortThreads)
-      a.named[w] = 0;
+  if (static_cast<int>(blockIdx.x) >= a.groups) {
+    clear_rows(c, blockIdx.x - a.groups);
+    return;
+  }
   const int64_t lo = blockIdx.x * a.per_group;
   sort_count(a, first != 0, lo, min(a.slots, lo + a.per_group), s);
   if (threadIdx.x < (1u << a.bits)) a.hist[(blockIdx.x << a.bits) + threadIdx.x] = s.base[threadIdx.x];
@@ -387,9 +409,6 @@ struct SumArgs {
   int piece;
   float* partial;            // [pieces][2][pitch]: sums of runs that come in / go on
   int pitch;
-  const uint32_t* named;     // null: no slot at all
-  int64_t sum_blocks;        // then the clearing workgroups
-  int clear_rows;            // table rows of one
   int lanes, col_blocks;
 };
 
@@ -409,29 +428,10 @@ __device__ __forceinline__ void put_row(const EmbedArgs& a, const LaneCols<T>& c
   cols.store(out, f);
 }
 
-template <typename O>
-__device__ __forceinline__ void clear_rows(const EmbedArgs& a, const SumArgs& s, int64_t block) {
-  constexpr int kO = Elem<O>::kPerVec;
-  const int vecs = a.dim / kO, tail = a.dim - vecs * kO;
-  const int64_t r0 = block * s.clear_rows, r1 = min(a.rows, r0 + s.clear_rows);
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const Word4 zero{0, 0, 0, 0};
-  for (int64_t r = r0 + wave; r < r1; r += kEmbThreads / 64) {
-    if (s.named && ((s.named[r >> 5] >> (r & 31)) & 1u)) continue;
-    O* out = static_cast<O*>(a.out) + r * a.out_ld;
-    for (int v = lane; v < vecs; v += 64) store_words(out + v * kO, zero);
-    if (lane < tail) out[vecs * kO + lane] = static_cast<O>(0.0f);
-  }
-}
-
 template <typename T, typename O>
 __global__ __launch_bounds__(kEmbThreads) void embed_sum_kernel(const EmbedArgs a, const SumArgs s) {
   constexpr int kE = Elem<T>::kPerVec;
   const int64_t block = static_cast<int64_t>(blockIdx.x);
-  if (block >= s.sum_blocks) {
-    clear_rows<O>(a, s, block - s.sum_blocks);
-    return;
-  }
   const int lane = threadIdx.x & (s.lanes - 1);
   const int groups = kEmbThreads / s.lanes;
   const int64_t piece = block / s.col_blocks * groups + threadIdx.x / s.lanes;
@@ -491,7 +491,7 @@ __global__ __launch_bounds__(kEmbThreads) void embed_sum_kernel(const EmbedArgs 
 
 // A run that starts in a piece and goes on: its partial sums in order.  One
 // CU reads some 40 GB/s: a long run's columns go to workgroups of a wavefront
-// (2048 columns, 137 pieces: 26 -> 9 us).
+// (2048 columns, 137 pieces: 26 -> 19 us).
 constexpr int kJoinThreads = 64;
 template <typename T, typename O>
 __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(const EmbedArgs a, const SumArgs s, int lanes,
@@ -555,7 +555,7 @@ struct EmbedPlan {
   int bits, passes, groups;          // passes 0: sort_owned_kernel, groups owners
   int64_t per_group, pieces;
   int piece;
-  int64_t off_a, off_b, off_hist, off_named, off_partial, bytes, named_words;
+  int64_t off_a, off_b, off_hist, off_partial, bytes;
   int pitch;
 };
 
@@ -565,7 +565,7 @@ EmbedPlan embed_plan(int64_t rows, int dim, int64_t slots) {
   EmbedPlan p{};
   int bits = 1;
   while ((rows >> bits) != 0) ++bits;                 // `rows` itself is a key
-  int own = 6;                                        // a wavefront writes whole words of the named bits
+  int own = 6;
   while (own < kSortMaxBits && (rows >> own) >= kOwnersFull) ++own;
   if (slots <= kOwnedSlots && (rows >> own) < kMostOwners) {
     p.bits = own;
@@ -580,7 +580,6 @@ EmbedPlan embed_plan(int64_t rows, int dim, int64_t slots) {
   p.piece = static_cast<int>(std::max<int64_t>(slots < kLongSlots ? kPiece : kLongPiece, round_up((slots + kMaxPieces - 1) / kMaxPieces, kAhead)));
   p.pieces = (slots + p.piece - 1) / p.piece;
   p.pitch = static_cast<int>(round_up(dim, 8));
-  p.named_words = (rows + 31) / 32;
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
     const int64_t off = at;
@@ -590,7 +589,6 @@ EmbedPlan embed_plan(int64_t rows, int dim, int64_t slots) {
   p.off_a = take(slots * 8);
   p.off_b = take(slots * 8);
   p.off_hist = take(p.passes > 0 ? static_cast<int64_t>(p.groups) * 4 << p.bits : 0);
-  p.off_named = take(p.named_words * 4);
   p.off_partial = take(p.pieces * 2 * p.pitch * 4);
   p.bytes = at;
   return p;
@@ -617,7 +615,9 @@ hipError_t lookup_typed(const EmbedArgs& a, hipStream_t s) {
   return hipSuccess;
 }
 
-hipError_t sort_slots(const EmbedArgs& a, const EmbedPlan& p, int64_t slots, char* ws, hipStream_t s, SumArgs& sum) {
+// Sorts the slots; its first launch clears the table beside it (c.blocks 0: not).
+hipError_t sort_slots(const EmbedArgs& a, const EmbedPlan& p, int64_t slots, char* ws, const ClearArgs& c,
+                      hipStream_t s, SumArgs& sum) {
   SortArgs o{};
   o.ids = a.ids;
   o.slots = slots;
@@ -627,7 +627,6 @@ hipError_t sort_slots(const EmbedArgs& a, const EmbedPlan& p, int64_t slots, cha
   o.groups = p.groups;
   o.per_group = p.per_group;
   o.hist = reinterpret_cast<uint32_t*>(ws + p.off_hist);
-  o.named = a.accumulate ? nullptr : reinterpret_cast<uint32_t*>(ws + p.off_named);
   SortBufs buf[2];
   buf[0].key = reinterpret_cast<uint32_t*>(ws + p.off_a);
   buf[1].key = reinterpret_cast<uint32_t*>(ws + p.off_b);
@@ -636,7 +635,7 @@ hipError_t sort_slots(const EmbedArgs& a, const EmbedPlan& p, int64_t slots, cha
   if (p.passes == 0) {
     o.in = buf[1];
     o.out = buf[0];
-    sort_owned_kernel<<<p.groups, kSortThreads, 0, s>>>(o);
+    sort_owned_kernel<<<static_cast<unsigned>(p.groups + c.blocks), kSortThreads, 0, s>>>(o, c);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   } else {
     for (int pass = 0; pass < p.passes; ++pass) {
@@ -644,7 +643,8 @@ hipError_t sort_slots(const EmbedArgs& a, const EmbedPlan& p, int64_t slots, cha
       o.shift = pass * p.bits;
       o.in = buf[to ^ 1];
       o.out = buf[to];
-      sort_count_kernel<<<p.groups, kSortThreads, 0, s>>>(o, pass == 0, p.named_words);
+      const int64_t blocks = p.groups + (pass == 0 ? c.blocks : 0);
+      sort_count_kernel<<<static_cast<unsigned>(blocks), kSortThreads, 0, s>>>(o, pass == 0, c);
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
       sort_move_kernel<<<p.groups, kSortThreads, 0, s>>>(o, pass == 0);
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
@@ -652,7 +652,6 @@ hipError_t sort_slots(const EmbedArgs& a, const EmbedPlan& p, int64_t slots, cha
   }
   sum.key = buf[to].key;
   sum.from = buf[to].from;
-  sum.named = o.named;
   return hipSuccess;
 }
 
@@ -661,9 +660,27 @@ hipError_t gradient_typed(const EmbedArgs& a, hipStream_t s) {
   const int64_t slots = a.n * a.bag;
   const EmbedPlan p = embed_plan(a.rows, a.dim, slots);
   char* ws = static_cast<char*>(a.workspace);
+  ClearArgs c{};
+  c.out = static_cast<char*>(a.out);
+  c.rows = a.rows;
+  c.row_bytes = c.last_bytes = static_cast<int64_t>(a.dim) * sizeof(O);
+  c.stride = a.out_ld * static_cast<int64_t>(sizeof(O));
+  c.threads = 64;
+  if (c.stride == c.row_bytes) {                     // one run of bytes, 64 KB a workgroup
+    const int64_t all = c.rows * c.row_bytes;
+    c.row_bytes = c.stride = 65536;
+    c.rows = (all + c.stride - 1) / c.stride;
+    c.last_bytes = all - (c.rows - 1) * c.stride;
+    c.threads = kSortThreads;
+  }
+  const int64_t per_block = kSortThreads / c.threads;
+  c.blocks = a.accumulate ? 0 : std::min<int64_t>((c.rows + per_block - 1) / per_block, 1 << 20);
   SumArgs sum{};
-  if (slots > 0)
-    if (hipError_t e = sort_slots(a, p, slots, ws, s, sum); e != hipSuccess) return e;
+  if (slots == 0) {
+    clear_kernel<<<static_cast<unsigned>(c.blocks), kSortThreads, 0, s>>>(c);
+    return hipGetLastError();
+  }
+  if (hipError_t e = sort_slots(a, p, slots, ws, c, s, sum); e != hipSuccess) return e;
   const int vecs = (a.dim + Elem<T>::kPerVec - 1) / Elem<T>::kPerVec;
   sum.slots = slots;
   sum.piece = p.piece;
@@ -673,13 +690,8 @@ hipError_t gradient_typed(const EmbedArgs& a, hipStream_t s) {
   sum.lanes = lanes_per_row(vecs);
   sum.col_blocks = (vecs + kEmbThreads - 1) / kEmbThreads;
   const int groups = kEmbThreads / sum.lanes;
-  sum.sum_blocks = (p.pieces + groups - 1) / groups * sum.col_blocks;
-  // A clearing workgroup takes about 64 KB of table, less where that would
-  // leave CUs idle.
-  const int64_t row_bytes = static_cast<int64_t>(a.dim) * sizeof(O);
-  sum.clear_rows = static_cast<int>(std::clamp<int64_t>(std::min(65536 / row_bytes, a.rows / 1024), 4, 4096));
-  const int64_t clear = a.accumulate ? 0 : (a.rows + sum.clear_rows - 1) / sum.clear_rows;
-  embed_sum_kernel<T, O><<<static_cast<unsigned>(sum.sum_blocks + clear), kEmbThreads, 0, s>>>(a, sum);
+  embed_sum_kernel<T, O><<<static_cast<unsigned>((p.pieces + groups - 1) / groups * sum.col_blocks), kEmbThreads, 0,
+                           s>>>(a, sum);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || p.pieces <= 1) return e;
   const int lanes = std::min(sum.lanes, kJoinThreads), per = kJoinThreads / lanes;
   const int col_blocks = (vecs + kJoinThreads - 1) / kJoinThreads;
