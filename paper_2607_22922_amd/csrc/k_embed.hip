@@ -392,12 +392,12 @@ __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(const SortArgs 
 }
 
 // ------------------------------------------------------------ summing runs
-// Sorted slots of a piece: few slots need many pieces to fill the GPU, many
-// slots fewer partial sums (32768 slots, a row of 13% of them: joining 19 -> 11
-// us); kMaxPieces bounds the longest join.
-constexpr int kPiece = 32;
-constexpr int kLongPiece = 64;
-constexpr int64_t kLongSlots = 1 << 14;
+// Sorted slots of a piece: about kPieces of them fill the GPU (512 slots: 10 ->
+// 4 us against pieces of 32), up to kLongPiece slots each (32768 slots, a row
+// of 13% of them: joining 19 us at 32, 11 at 64); kMaxPieces bounds the
+// longest join.
+constexpr int64_t kPieces = 512;
+constexpr int64_t kLongPiece = 64;
 constexpr int64_t kMaxPieces = 1 << 13;
 constexpr int kAhead = 8;                  // gradient rows in flight per lane
 
@@ -457,24 +457,33 @@ __global__ __launch_bounds__(kEmbThreads) void embed_sum_kernel(const EmbedArgs 
       put_row<O>(a, cols, run, sum);
     }
   };
-  for (int64_t at = lo; at < hi; at += kAhead) {
-    // Absent slots' rows are read too (their run is dropped), and past the
-    // end the last slot's again: no load waits for a branch.
-    uint32_t key[kAhead], from[kAhead];
-    Word4 w[kAhead];
+  // Absent slots' rows are read too (their run is dropped), and past the end
+  // the last slot's again: no load waits for a branch.  A step's keys are read
+  // during the step before it.
+  uint32_t key[kAhead], from[kAhead];
+  auto read_keys = [&](int64_t at) {
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       key[u] = s.key[min(at + u, hi - 1)];
       from[u] = s.from[min(at + u, hi - 1)];
     }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) w[u] = cols.load_raw(grad + static_cast<int64_t>(from[u]) * a.grad_ld);
+  };
+  read_keys(lo);
+  for (int64_t at = lo; at < hi; at += kAhead) {
+    Word4 w[kAhead];
+    uint32_t now[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      if (key[u] != run && at + u < hi) {
+      w[u] = cols.load_raw(grad + static_cast<int64_t>(from[u]) * a.grad_ld);
+      now[u] = key[u];
+    }
+    read_keys(at + kAhead);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (now[u] != run && at + u < hi) {
         flush(false);
         came_in = false;
-        run = key[u];
+        run = now[u];
 #pragma unroll
         for (int e = 0; e < kE; ++e) sum[e] = 0.0f;
       }
@@ -577,7 +586,9 @@ EmbedPlan embed_plan(int64_t rows, int dim, int64_t slots) {
     p.per_group = (tiles + kSortMaxGroups - 1) / kSortMaxGroups * kSortTile;
     p.groups = static_cast<int>((slots + p.per_group - 1) / p.per_group);
   }
-  p.piece = static_cast<int>(std::max<int64_t>(slots < kLongSlots ? kPiece : kLongPiece, round_up((slots + kMaxPieces - 1) / kMaxPieces, kAhead)));
+  p.piece = static_cast<int>(round_up(
+      std::max({std::min((slots + kPieces - 1) / kPieces, kLongPiece), (slots + kMaxPieces - 1) / kMaxPieces, int64_t{1}}),
+      kAhead));
   p.pieces = (slots + p.piece - 1) / p.piece;
   p.pitch = static_cast<int>(round_up(dim, 8));
   int64_t at = 0;
