@@ -66,9 +66,19 @@ __device__ __forceinline__ Stat join(const Stat& a, const Stat& b) {
   return {o, sa + sb, wa + wb};
 }
 
+// Joins the sums that a wavefront's lanes hold (sum 0: none), in every lane.
+__device__ __forceinline__ Stat join_lanes(const Stat& mine) {
+  const bool any = mine.sum != 0.0;
+  const double o = wave_max(any ? mine.origin : -INFINITY);
+  const double d = any ? mine.origin - o : 0.0;
+  const double sum = any ? times_pow2(mine.sum, d) : 0.0;
+  const double wsum = sum == 0.0 ? 0.0 : times_pow2(mine.wsum, d) + d * sum;
+  return {o, wave_add(sum), wave_add(wsum)};
+}
+
 // The sums of a wavefront's elements, in every lane.
 template <bool kEntropy, typename T, int kThreads, int kVecs>
-__device__ __forceinline__ Stat wave_stat(RowTile<T, kThreads, kVecs>& tile, float mx, float c) {
+__device__ __forceinline__ Stat wave_stat(RowTile<T, kThreads, kVecs>& tile, const T* x, float mx, float c) {
   constexpr int kE = Elem<T>::kPerVec;
   tile.forget_unpacked();
   float sum = 0.0f, wsum = 0.0f;
@@ -76,8 +86,8 @@ __device__ __forceinline__ Stat wave_stat(RowTile<T, kThreads, kVecs>& tile, flo
   const float b = mx == -INFINITY ? 0.0f : rintf(mx * c);
   if (fabsf(b) < kHuge) {
     origin = b;
-    auto add = [&](float x) {
-      const float z = __fmaf_rn(x, c, -b);
+    auto add = [&](float v) {
+      const float z = __fmaf_rn(v, c, -b);
       const float e = exp2_fast(z);
       sum += e;
       if constexpr (kEntropy) wsum = __fmaf_rn(e, fmaxf(z, kExpFloor), wsum);
@@ -94,17 +104,7 @@ __device__ __forceinline__ Stat wave_stat(RowTile<T, kThreads, kVecs>& tile, flo
     add(tile.tail);
   } else {
     origin = static_cast<double>(mx) * c;
-    auto add = [&](float x) { sum += x == mx ? 1.0f : (isnan(x) || x == INFINITY ? NAN : 0.0f); };
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i)
-      if (tile.has(i)) {
-        float f[kE];
-        Elem<T>::unpack(tile.v[i], f);
-#pragma unroll
-        for (int j = 0; j < kE; ++j) add(f[j]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    add(tile.tail);
+    tile.each_from_memory(x, [&](float v, int) { sum += v == mx ? 1.0f : (isnan(v) ? NAN : 0.0f); });
     if (mx == INFINITY) sum = NAN;
   }
   return {origin, wave_add(static_cast<double>(sum)), kEntropy ? wave_add(static_cast<double>(wsum)) : 0.0};
@@ -299,7 +299,7 @@ __global__ __launch_bounds__(kThreads, 4) void log_probs_tile_kernel(const LogPr
   RowTile<T, kThreads, kVecs> tile;
   tile.load(x + first, mine);
   const float tmax = tile.thread_max();
-  Stat st = wave_stat<true>(tile, wave_max(tmax), static_cast<float>(a.c));
+  Stat st = wave_stat<true>(tile, x + first, wave_max(tmax), static_cast<float>(a.c));
   if constexpr (kWaves > 1) {
     if ((tid & 63) == 0) s_stat[wave] = st;
     __syncthreads();
@@ -345,9 +345,7 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(const LogProbArgs a,
   uint64_t head = 0;
   const uint64_t* list = keys + (row * chunks + (lane < chunks ? lane : 0)) * a.n_top;
   if (a.n_top > 0 && lane < chunks) head = list[0];
-  Stat st{lane_of(mine.origin, 0), lane_of(mine.sum, 0), lane_of(mine.wsum, 0)};
-  for (int j = 1; j < chunks; ++j)
-    st = join(st, Stat{lane_of(mine.origin, j), lane_of(mine.sum, j), lane_of(mine.wsum, j)});
+  const Stat st = join_lanes(mine);
   const RowProb p(st, static_cast<float>(a.c));
   const T* x = static_cast<const T*>(a.logits) + row * a.ld;
   if (lane == 0 && a.entropy_out) a.entropy_out[row] = p.entropy(st);
@@ -401,13 +399,19 @@ struct DistillStat {
   double other_origin, other_sum, named_origin, named_sum, loss, psum;
 };
 
-// What the row's gradient needs: an other column has coef 2^(x c - origin), a
-// named one weight tau (2^(x c - origin - lse2) - p).
+// What the others' gradient needs, cheap to compute while the tile is held: an
+// other column has coef 2^(x c - origin).
 constexpr int kRowNan = 1, kRowFinite = 2;        // 0: loss and gradient 0
 struct DistillRow {
-  double origin, lse2;
-  float coef, loss;
+  double origin, hi, all;      // all columns' sum is 2^hi all
+  float coef;
   int mode;
+};
+
+// What takes logarithms: a named column has weight tau (2^(x c - hi - log2_all) - p).
+struct DistillEnd {
+  double log2_all;
+  float loss;
 };
 
 // Dynamic LDS of the distillation: per slot the column relative to the chunk
@@ -496,7 +500,7 @@ __device__ __forceinline__ DistillStat named_stat(const DistillArgs& a, int64_t 
       mx = fmax(mx, x * a.c);
     }
   mx = wave_max(mx);
-  if (mx == -INFINITY) mx = 0.0;
+  mx = mx == -INFINITY ? 0.0 : rint(mx);           // whole: sums join by exact powers of two
   double sum = 0.0, loss = 0.0, psum = 0.0;
   for (int k = lane; k < a.n_teacher; k += 64) {
     const int column = t.column[k];
@@ -514,25 +518,22 @@ __device__ __forceinline__ DistillStat named_stat(const DistillArgs& a, int64_t 
   return {0.0, 0.0, mx, __any(bad) ? NAN : sum, wave_add(loss), wave_add(psum)};
 }
 
-// Joins the statistics that a wavefront's first `count` lanes hold, in every lane.
-__device__ __forceinline__ DistillStat join_lanes(DistillStat st, int count) {
-  const int lane = threadIdx.x & 63;
-  const bool other = lane < count && st.other_sum != 0.0;
-  const double o = wave_max(other ? st.other_origin : -INFINITY);
-  st.other_sum = wave_add(other ? times_pow2(st.other_sum, st.other_origin - o) : 0.0);
-  st.other_origin = o;
-  const bool named = lane < count && (st.named_sum != 0.0 || st.psum != 0.0);
-  const double m = wave_max(named ? st.named_origin : -INFINITY);
-  const double d = named ? st.named_origin - m : 0.0;
-  // sum p (log p - ln 2 (x c - m)) from the chunk's own origin
-  st.loss = wave_add(named ? (st.psum == 0.0 ? 0.0 : st.loss - st.psum * d * kLn2) : 0.0);
-  st.named_sum = wave_add(named ? st.named_sum * pow2(d) : 0.0);
-  st.psum = wave_add(named ? st.psum : 0.0);
+// Joins the statistics that a wavefront's lanes hold, in every lane.
+__device__ __forceinline__ DistillStat join_lanes(const DistillStat& mine) {
+  const Stat other = join_lanes(Stat{mine.other_origin, mine.other_sum, 0.0});
+  DistillStat st{other.origin, other.sum, 0.0, 0.0, 0.0, 0.0};
+  const bool named = mine.named_sum != 0.0 || mine.psum != 0.0;
+  const double m = wave_max(named ? mine.named_origin : -INFINITY);
+  const double d = named ? mine.named_origin - m : 0.0;
   st.named_origin = m;
+  st.named_sum = wave_add(named ? times_pow2(mine.named_sum, d) : 0.0);
+  // sum p (log p - ln 2 (x c - m)) from the chunk's own origin
+  st.loss = wave_add(mine.psum == 0.0 ? 0.0 : mine.loss - mine.psum * d * kLn2);
+  st.psum = wave_add(mine.psum);
   return st;
 }
 
-// From the whole row's sums: its loss, and what the gradient needs.
+// From the whole row's sums.
 __device__ __forceinline__ DistillRow distill_row(const DistillArgs& a, const DistillStat& st, const Teacher& teacher,
                                                   float weight) {
   DistillRow r{};
@@ -540,36 +541,44 @@ __device__ __forceinline__ DistillRow distill_row(const DistillArgs& a, const Di
   const bool other = st.other_sum != 0.0, named = st.named_sum != 0.0;
   if (teacher.bad || isnan(st.other_sum) || isnan(st.named_sum)) {
     r.mode = kRowNan;
-    r.loss = NAN;
     return r;
   }
   if (!other && !named) return r;                                     // no distribution
-  const double hi = fmax(other ? st.other_origin : -INFINITY, named ? st.named_origin : -INFINITY);
-  const double all = (other ? st.other_sum * pow2(st.other_origin - hi) : 0.0) +
-                     (named ? st.named_sum * pow2(st.named_origin - hi) : 0.0);
+  r.hi = fmax(other ? st.other_origin : -INFINITY, named ? st.named_origin : -INFINITY);
+  const double others = other ? times_pow2(st.other_sum, st.other_origin - r.hi) : 0.0;
+  r.all = others + (named ? times_pow2(st.named_sum, st.named_origin - r.hi) : 0.0);
   r.mode = kRowFinite;
-  r.origin = other ? st.other_origin : hi;
-  const double log2_all = log2(all);
-  r.lse2 = (hi - r.origin) + log2_all;
-  double loss = st.psum > 0.0 ? st.loss + st.psum * ((hi - st.named_origin) + log2_all) * kLn2 : 0.0;
-  if (other) {
-    const double log2_q = log2(st.other_sum) - r.lse2;                // of the others' share Q
-    if (teacher.rest > 0.0) loss += teacher.rest * (log(teacher.rest) - log2_q * kLn2);
-    r.coef = static_cast<float>(static_cast<double>(weight) * a.tau * (exp2(log2_q) - teacher.rest) / st.other_sum);
-  }
-  r.loss = static_cast<float>(loss * (static_cast<double>(a.tau) * a.tau));
+  r.origin = other ? st.other_origin : r.hi;
+  // Q = others / all
+  if (other)
+    r.coef = static_cast<float>(static_cast<double>(weight) * a.tau * (others / r.all - teacher.rest) / st.other_sum);
   return r;
+}
+
+__device__ __forceinline__ DistillEnd distill_end(const DistillArgs& a, const DistillRow& r, const DistillStat& st,
+                                                  const Teacher& teacher) {
+  if (r.mode != kRowFinite) return {0.0, r.mode == kRowNan ? NAN : 0.0f};
+  DistillEnd e;
+  e.log2_all = log2(r.all);
+  double loss = st.psum > 0.0 ? st.loss + st.psum * ((r.hi - st.named_origin) + e.log2_all) * kLn2 : 0.0;
+  if (st.other_sum != 0.0 && teacher.rest > 0.0)
+    loss += teacher.rest *
+            (log(teacher.rest) - ((st.other_origin - r.hi) + (log2(st.other_sum) - e.log2_all)) * kLn2);
+  e.loss = static_cast<float>(loss * (static_cast<double>(a.tau) * a.tau));
+  return e;
 }
 
 // The other columns' sum in a wavefront's registers, in every lane.
 template <typename T, int kThreads, int kVecs>
-__device__ __forceinline__ void other_stat(RowTile<T, kThreads, kVecs>& tile, float mx, const DistillArgs& a,
-                                           DistillStat& st) {
+__device__ __forceinline__ Stat other_stat(RowTile<T, kThreads, kVecs>& tile, const T* x, const unsigned char* bits,
+                                           float mx, const DistillArgs& a) {
   constexpr int kE = Elem<T>::kPerVec;
   const SplitC c = split_c(a.c);
   const float b = mx == -INFINITY ? 0.0f : rintf(mx * c.hi);
   float sum = 0.0f;
-  auto each = [&](auto&& add) {
+  double origin = b;
+  if (fabsf(b) < kHuge) {
+    auto add = [&](float v) { sum += exp2_fast(__fmaf_rn(v, c.lo, __fmaf_rn(v, c.hi, -b))); };
     tile.forget_unpacked();
 #pragma unroll
     for (int i = 0; i < kVecs; ++i)
@@ -581,16 +590,15 @@ __device__ __forceinline__ void other_stat(RowTile<T, kThreads, kVecs>& tile, fl
         __builtin_amdgcn_sched_barrier(0);
       }
     add(tile.tail);
-  };
-  if (fabsf(b) < kHuge) {
-    st.other_origin = b;
-    each([&](float x) { sum += exp2_fast(__fmaf_rn(x, c.lo, __fmaf_rn(x, c.hi, -b))); });
   } else {
-    st.other_origin = mx * a.c;
-    each([&](float x) { sum += x == mx ? 1.0f : (isnan(x) ? NAN : 0.0f); });
+    origin = mx * a.c;
+    tile.each_from_memory(x, [&](float v, int column) {
+      if ((bits[column / kE] >> (column % kE)) & 1u) return;
+      sum += v == mx ? 1.0f : (isnan(v) ? NAN : 0.0f);
+    });
     if (mx == INFINITY) sum = NAN;
   }
-  st.other_sum = wave_add(static_cast<double>(sum));
+  return {origin, wave_add(static_cast<double>(sum)), 0.0};
 }
 
 // n elements of g at p.
@@ -606,64 +614,99 @@ __device__ __forceinline__ void fill_range(T* p, int n, float g, int tid, int th
   for (int v = nvec * kE + tid; v < n; v += threads) p[v] = elem_round<T>(g);
 }
 
-// The gradient of a chunk: `mine` columns of the tile, zeros up to `cols`.
-// Every column is written as another one, then, after a barrier, the named
-// ones anew (wave stores to one address stay in order once they have left).
+// The gradient of the tile's columns, every one as an other one.
 template <typename T, int kThreads, int kVecs>
-__device__ __forceinline__ void write_gradient(RowTile<T, kThreads, kVecs>& tile, const DistillArgs& a,
-                                               const DistillRow& r, float weight, const TeacherLds& t, T* grad, int mine,
-                                               int cols) {
+__device__ __forceinline__ void write_others(RowTile<T, kThreads, kVecs>& tile, const DistillArgs& a,
+                                             const DistillRow& r, const T* x, T* grad) {
   constexpr int kE = Elem<T>::kPerVec;
   const int tid = threadIdx.x;
-  fill_range(grad + mine, cols - mine, 0.0f, tid, kThreads);
-  if (r.mode != kRowFinite) {
-    fill_range(grad, mine, r.mode == kRowNan ? NAN : 0.0f, tid, kThreads);
-    return;
-  }
   const SplitC c = split_c(a.c);
   const float coef = r.coef;
-  auto each = [&](auto&& fn) {
-    tile.forget_unpacked();
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i)
-      if (tile.has(i)) {
-        const int at = i * kThreads + tid;
-        if (at < tile.nvec) {
-          float f[kE];
-          Elem<T>::unpack(tile.v[i], f);
-#pragma unroll
-          for (int j = 0; j < kE; ++j) f[j] = fn(f[j]);
-          store_words(reinterpret_cast<char*>(grad) + static_cast<uint32_t>(at) * 16u, Elem<T>::pack(f));
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    if (tid < tile.ntail) grad[tile.tail_column()] = elem_round<T>(fn(tile.tail));
-  };
-  if (fabs(r.origin) < kHuge) {
-    const float b = static_cast<float>(r.origin);
-    each([&](float x) { return coef * exp2_fast(__fmaf_rn(x, c.lo, __fmaf_rn(x, c.hi, -b))); });
-  } else {
-    each([&](float x) { return x * a.c == r.origin ? coef : 0.0f; });
+  if (fabs(r.origin) >= kHuge) {
+    tile.each_from_memory(x, [&](float v, int column) { grad[column] = elem_round<T>(v * a.c == r.origin ? coef : 0.0f); });
+    return;
   }
+  const float b = static_cast<float>(r.origin);
+  auto gradient = [&](float v) { return coef * exp2_fast(__fmaf_rn(v, c.lo, __fmaf_rn(v, c.hi, -b))); };
+  tile.forget_unpacked();
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i)
+    if (tile.has(i)) {
+      if (tid < tile.nvec - i * kThreads) {
+        float f[kE];
+        Elem<T>::unpack(tile.v[i], f);
+#pragma unroll
+        for (int j = 0; j < kE; ++j) f[j] = gradient(f[j]);
+        char* to = reinterpret_cast<char*>(grad) + static_cast<int64_t>(i) * kThreads * 16;
+        store_words(to + tid * 16u, Elem<T>::pack(f));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  if (tid < tile.ntail) grad[tile.tail_column()] = elem_round<T>(gradient(tile.tail));
+}
+
+// After the tile: the loss, and the named columns' gradient over what
+// write_others has put there (the workgroup's stores have left when the
+// barrier opens, so these come last).  grad may be null.
+template <typename T, int kThreads>
+__device__ __forceinline__ void finish_named(const DistillArgs& a, int64_t row, const DistillRow& r,
+                                             const DistillStat& st, const Teacher& teacher, float weight,
+                                             const TeacherLds& t, bool write_loss, T* grad, DistillEnd& s_end) {
+  const int tid = threadIdx.x;
+  if (tid < 64) {
+    const DistillEnd e = distill_end(a, r, st, teacher);
+    if (tid == 0) {
+      s_end = e;
+      if (write_loss) a.loss_out[row] = e.loss;
+    }
+  }
+  if (!grad || r.mode != kRowFinite) return;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   group_sync<kThreads>();
+  const double log2_all = s_end.log2_all;
   for (int k = tid; k < a.n_teacher; k += kThreads) {
     const int column = t.column[k];
     if (column < 0) continue;
     double p = 0.0;
     for (int o = 0; o < a.n_teacher; ++o) p += t.column[o] == column ? t.p[o] : 0.0;
-    const double q = pow2(t.x[k] * a.c - r.origin - r.lse2);
+    const double q = pow2(t.x[k] * a.c - r.hi - log2_all);
     grad[column] = elem_round<T>(static_cast<float>(static_cast<double>(weight) * a.tau * (q - p)));
   }
 }
 
-// The chunk's named columns' logits and bits, by the wavefront that read the
-// teacher; bits may be null.
+// Columns without a gradient: those past the row's length, and all of a row
+// that is left out or undefined (false: there is nothing else to write).
+template <typename T, int kThreads>
+__device__ __forceinline__ bool write_rest(const DistillRow& r, T* grad, int mine, int cols) {
+  const int tid = threadIdx.x;
+  fill_range(grad + mine, cols - mine, 0.0f, tid, kThreads);
+  if (r.mode == kRowFinite) return true;
+  fill_range(grad, mine, r.mode == kRowNan ? NAN : 0.0f, tid, kThreads);
+  return false;
+}
+
+// The named columns' logits, by the wavefront that read the teacher.
 template <typename T>
 __device__ __forceinline__ void gather_named(const DistillArgs& a, const T* x, const TeacherLds& t) {
   for (int k = threadIdx.x & 63; k < a.n_teacher; k += 64) {
     const int column = t.column[k];
     t.x[k] = column >= 0 ? elem_load(x + column) : -INFINITY;
+  }
+}
+
+// A bit for every named column of [first, first + columns), by one wavefront.
+template <typename T, int kThreads, int kVecs>
+__device__ __forceinline__ void mark_named(const DistillArgs& a, const TeacherLds& t, int first, int columns) {
+  constexpr int kBitWords = (kThreads * kVecs + 16) / 16;
+  const int lane = threadIdx.x & 63;
+  for (int w = lane; w < kBitWords; w += 64) reinterpret_cast<Word4*>(t.bits)[w] = Word4{0, 0, 0, 0};
+  group_sync<64>();
+  for (int k = lane; k < a.n_teacher; k += 64) {
+    const int column = t.column[k] - first;
+    if (t.column[k] >= 0 && column >= 0 && column < columns) {
+      const int vec = column / Elem<T>::kPerVec;
+      atomicOr(reinterpret_cast<unsigned*>(t.bits) + (vec >> 2), 1u << (8 * (vec & 3) + column % Elem<T>::kPerVec));
+    }
   }
 }
 
@@ -687,15 +730,55 @@ __device__ __forceinline__ void drop_named(RowTile<T, kThreads, kVecs>& tile, co
   if (tid < tile.ntail && ((bits[tile.nvec] >> tid) & 1u)) tile.tail = -INFINITY;
 }
 
+// What the wavefront that reads the teacher leaves for the workgroup.
+struct TeacherState {
+  Teacher teacher;
+  DistillStat named;
+};
+
+template <typename T, int kThreads, int kVecs>
+__device__ __forceinline__ void teacher_state(const DistillArgs& a, int64_t row, const T* x, int len, int first,
+                                              int mine, const TeacherLds& t, TeacherState& s) {
+  const Teacher teacher = read_teacher(a, row, len, first, mine, t);
+  gather_named(a, x, t);
+  const DistillStat named = named_stat(a, row, t, teacher);
+  if ((threadIdx.x & 63) == 0) s = {teacher, named};
+}
+
+// Joins the wavefronts' sums of the others to the named columns' in
+// s.named, and leaves the row's gradient data in s_row (whole rows).  Two
+// barriers.
+template <int kThreads>
+__device__ __forceinline__ void join_row(const DistillArgs& a, float weight, const Stat& other, Stat* s_stat,
+                                         TeacherState& s, DistillRow* s_row) {
+  constexpr int kWaves = kThreads / 64;
+  const int tid = threadIdx.x;
+  if (kWaves > 1 && (tid & 63) == 0) s_stat[tid >> 6] = other;
+  group_sync<kThreads>();
+  if (tid < 64) {
+    DistillStat st = s.named;
+    const Stat all = kWaves > 1 ? join_lanes(tid < kWaves ? s_stat[tid] : Stat{0.0, 0.0, 0.0}) : other;
+    st.other_origin = all.origin;
+    st.other_sum = all.sum;
+    if (tid == 0) s.named = st;
+    if (s_row) {
+      const DistillRow r = distill_row(a, st, s.teacher, weight);
+      if (tid == 0) *s_row = r;
+    }
+  }
+  group_sync<kThreads>();
+}
+
 // One workgroup per row (kWhole: chunks is 1, loss and gradient are written)
 // or per (row, chunk), whose sums go to the workspace.
 template <typename T, int kThreads, int kVecs, bool kWhole>
-__global__ __launch_bounds__(kThreads, 4) void distill_tile_kernel(
-    const DistillArgs a, int64_t item0, int chunk, int chunks, DistillStat* stats) {
+__global__ __launch_bounds__(kThreads, 4) void distill_tile_kernel(const DistillArgs a, int64_t item0, int chunk,
+                                                                   int chunks, DistillStat* stats) {
   extern __shared__ __align__(16) unsigned char smem[];
-  constexpr int kWaves = kThreads / 64;
-  __shared__ DistillStat s_stat[kWaves];
+  __shared__ Stat s_stat[kThreads / 64];
   __shared__ DistillRow s_row;
+  __shared__ DistillEnd s_end;
+  __shared__ TeacherState s_teacher;
   const int tid = threadIdx.x;
   const int64_t item = item0 + blockIdx.x;
   const int64_t row = kWhole ? item : item / chunks;
@@ -714,50 +797,78 @@ __global__ __launch_bounds__(kThreads, 4) void distill_tile_kernel(
   const int mine = kWhole ? len : max(0, min(chunk, len - first));
   const TeacherLds t = teacher_lds(smem, a.n_teacher);
   RowTile<T, kThreads, kVecs> tile;
-  tile.load(x, mine);
-  Teacher teacher{};
-  DistillStat st{};
+  // The teacher's wavefront has no registers for its mathematics beside a
+  // large tile: it reads its part of the row afterwards.
+  constexpr bool kTeacherFirst = kVecs > 8;
+  if (!kTeacherFirst) tile.load(x, mine);
   if (tid < 64) {
-    constexpr int kBitWords = (kThreads * kVecs + 16) / 16;
-    for (int w = tid; w < kBitWords; w += 64) reinterpret_cast<Word4*>(t.bits)[w] = Word4{0, 0, 0, 0};
-    teacher = read_teacher(a, row, len, first, mine, t);
-    gather_named(a, x, t);
-    for (int k = tid; k < a.n_teacher; k += 64) {
-      const int column = t.column[k];
-      if (column >= 0) {
-        const int vec = column / Elem<T>::kPerVec;
-        atomicOr(reinterpret_cast<unsigned*>(t.bits) + (vec >> 2), 1u << (8 * (vec & 3) + column % Elem<T>::kPerVec));
-      }
-    }
-    st = named_stat(a, row, t, teacher);
+    teacher_state<T, kThreads, kVecs>(a, row, x, len, first, mine, t, s_teacher);
+    mark_named<T, kThreads, kVecs>(a, t, 0, mine);
   }
+  if (kTeacherFirst) tile.load(x, mine);
   group_sync<kThreads>();
   drop_named(tile, t.bits);
-  DistillStat mine_st{};
-  other_stat(tile, wave_max(tile.thread_max()), a, mine_st);
-  if constexpr (kWaves > 1) {
-    if ((tid & 63) == 0) s_stat[tid >> 6] = mine_st;
-    __syncthreads();
+  const Stat other = other_stat(tile, x, t.bits, wave_max(tile.thread_max()), a);
+  join_row<kThreads>(a, weight, other, s_stat, s_teacher, kWhole ? &s_row : nullptr);
+  if constexpr (kWhole) {
+    const DistillRow r = s_row;
+    T* grad = a.grad_out ? static_cast<T*>(a.grad_out) + row * a.grad_ld : nullptr;
+    if (grad && write_rest<T, kThreads>(r, grad, mine, cols)) write_others(tile, a, r, x, grad);
+    finish_named<T, kThreads>(a, row, r, s_teacher.named, s_teacher.teacher, weight, t, true, grad, s_end);
+  } else if (tid == 0) {
+    stats[item] = s_teacher.named;
   }
-  if (tid < 64) {
-    if constexpr (kWaves > 1) mine_st = join_lanes(tid < kWaves ? s_stat[tid] : DistillStat{}, kWaves);
-    st.other_origin = mine_st.other_origin;
-    st.other_sum = mine_st.other_sum;
-    if constexpr (kWhole) {
-      const DistillRow r = distill_row(a, st, teacher, weight);
-      if (tid == 0) {
-        s_row = r;
-        a.loss_out[row] = r.loss;
-      }
-    } else if (tid == 0) {
-      stats[item] = st;
+}
+
+// A workgroup per row longer than its tile: the row's segments pass through
+// the tile from the last to the first, which stays; the others are read again
+// for the gradient (from the last-level cache: the rows in flight fit it).
+template <typename T, int kThreads, int kVecs>
+__global__ __launch_bounds__(kThreads) void distill_long_kernel(const DistillArgs a, int64_t row0) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ Stat s_stat[kThreads / 64];
+  __shared__ DistillRow s_row;
+  __shared__ DistillEnd s_end;
+  __shared__ TeacherState s_teacher;
+  using Tile = RowTile<T, kThreads, kVecs>;
+  const int tid = threadIdx.x;
+  const int64_t row = row0 + blockIdx.x;
+  const float weight = a.row_weight ? a.row_weight[row] : 1.0f;
+  const int cols = static_cast<int>(a.cols);
+  T* grad = a.grad_out ? static_cast<T*>(a.grad_out) + row * a.grad_ld : nullptr;
+  if (weight == 0.0f) {
+    if (tid == 0) a.loss_out[row] = 0.0f;
+    if (grad) fill_range(grad, cols, 0.0f, tid, kThreads);
+    return;
+  }
+  const T* x = static_cast<const T*>(a.logits) + row * a.ld;
+  const int mine = row_cols(a.n_valid, row, a.cols);
+  const TeacherLds t = teacher_lds(smem, a.n_teacher);
+  if (tid < 64) teacher_state<T, kThreads, kVecs>(a, row, x, mine, 0, mine, t, s_teacher);
+  Tile tile;
+  Stat other{0.0, 0.0, 0.0};
+  int at = mine > 0 ? (mine - 1) / Tile::kCapacity * Tile::kCapacity : 0;
+  for (;; at -= Tile::kCapacity) {
+    const int n = min(mine - at, Tile::kCapacity);
+    if (at > 0 && grad) tile.template load<false>(x + at, n);
+    else tile.load(x + at, n);
+    if (tid < 64) mark_named<T, kThreads, kVecs>(a, t, at, n);
+    __syncthreads();
+    drop_named(tile, t.bits);
+    other = join(other, other_stat(tile, x + at, t.bits, wave_max(tile.thread_max()), a));
+    if (at == 0) break;
+    __syncthreads();                                   // the segment's bits have been read
+  }
+  join_row<kThreads>(a, weight, other, s_stat, s_teacher, &s_row);
+  const DistillRow r = s_row;
+  if (grad && write_rest<T, kThreads>(r, grad, mine, cols)) {
+    write_others(tile, a, r, x, grad);
+    for (at = Tile::kCapacity; at < mine; at += Tile::kCapacity) {
+      tile.load(x + at, min(mine - at, Tile::kCapacity));
+      write_others(tile, a, r, x + at, grad + at);
     }
   }
-  if constexpr (kWhole) {
-    if (!a.grad_out) return;
-    group_sync<kThreads>();
-    write_gradient(tile, a, s_row, weight, t, static_cast<T*>(a.grad_out) + row * a.grad_ld, mine, cols);
-  }
+  finish_named<T, kThreads>(a, row, r, s_teacher.named, s_teacher.teacher, weight, t, true, grad, s_end);
 }
 
 // The second launch of rows in chunks: every workgroup joins its row's sums
@@ -769,6 +880,8 @@ __global__ __launch_bounds__(kThreads) void distill_join_kernel(const DistillArg
                                                                 const DistillStat* stats) {
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ DistillRow s_row;
+  __shared__ DistillEnd s_end;
+  __shared__ TeacherState s_teacher;
   const int tid = threadIdx.x;
   const int64_t item = item0 + blockIdx.x;
   const int64_t row = item / chunks_grid;
@@ -786,20 +899,22 @@ __global__ __launch_bounds__(kThreads) void distill_join_kernel(const DistillArg
   const int mine = max(0, min(chunk, len - first));
   const TeacherLds t = teacher_lds(smem, a.n_teacher);
   RowTile<T, kThreads, kVecs> tile;
-  if (grad) tile.load(x, mine);
   if (tid < 64) {
     const DistillStat own = tid < chunks ? stats[row * chunks + tid] : DistillStat{};
     const Teacher teacher = read_teacher(a, row, len, first, mine, t);
     if (grad) gather_named(a, x, t);
-    const DistillRow r = distill_row(a, join_lanes(own, chunks), teacher, weight);
+    const DistillStat st = join_lanes(own);
+    const DistillRow r = distill_row(a, st, teacher, weight);
     if (tid == 0) {
+      s_teacher = {teacher, st};
       s_row = r;
-      if (first == 0) a.loss_out[row] = r.loss;
     }
   }
-  if (!grad) return;
+  if (grad) tile.load(x, mine);
   group_sync<kThreads>();
-  write_gradient(tile, a, s_row, weight, t, grad, mine, cols);
+  const DistillRow r = s_row;
+  if (grad && write_rest<T, kThreads>(r, grad, mine, cols)) write_others(tile, a, r, x, grad);
+  finish_named<T, kThreads>(a, row, r, s_teacher.named, s_teacher.teacher, weight, t, first == 0, grad, s_end);
 }
 
 }  // namespace
@@ -810,18 +925,20 @@ struct RowPlan {
   int threads, vecs, chunk, chunks;
 };
 
-// A row goes to the smallest workgroup that holds it, a wavefront up to 512
-// vectors; longer rows, and rows too few to give every CU a workgroup, to
-// chunks of 256-thread workgroups.  A chunk of fewer than 256 vectors would
-// leave threads idle.
+// A row of up to 4096 vectors goes to the smallest workgroup that holds it (a
+// wavefront up to 512 vectors), longer rows to chunks of 256-thread
+// workgroups: enough of them to give every CU two, none of fewer than 256
+// vectors.  (One launch of few workgroups beats two launches that fill the
+// GPU: 256 rows of 28000 fp16 logits 17 us against 23.)
 RowPlan log_probs_plan(int64_t n, int64_t cols, int per_vec) {
-  constexpr int64_t kFill = 512;               // workgroups: two per CU
+  constexpr int64_t kFill = 512;
   const int64_t vecs = (cols + per_vec - 1) / per_vec;
   if (vecs <= 128) return {64, 2, static_cast<int>(cols), 1};
   if (vecs <= 512) return {64, 8, static_cast<int>(cols), 1};
+  if (vecs <= 4096) return {256, vecs <= 2048 ? 8 : 16, static_cast<int>(cols), 1};
   int64_t chunks = (vecs + 4095) / 4096;
-  if (n * chunks < kFill) chunks = std::min<int64_t>({(kFill + n - 1) / n, (vecs + 255) / 256, kMaxChunks});
-  if (chunks == 1) return {256, vecs <= 2048 ? 8 : 16, static_cast<int>(cols), 1};
+  if (n * chunks < kFill)
+    chunks = std::max(chunks, std::min<int64_t>({(kFill + n - 1) / n, (vecs + 255) / 256, kMaxChunks}));
   const int64_t chunk = (vecs + chunks - 1) / chunks;
   return {256, chunk <= 2048 ? 8 : 16, static_cast<int>(chunk * per_vec),
           static_cast<int>((vecs + chunk - 1) / chunk)};
@@ -878,11 +995,16 @@ hipError_t launch_log_probs(const LogProbArgs& a, hipStream_t s) {
   }
 }
 
-// As log_probs_plan, and rows of up to 16384 vectors to one workgroup of 1024
-// threads: it reads the logits once, where two launches read them twice.
+// As log_probs_plan, but where there is a row for every other CU a workgroup
+// takes a whole long row: it reads part of the logits once, where two launches
+// read all of them twice (131072 bf16 columns, 512 rows: 69 us against 98; 128
+// rows 36 and 35, 64 rows 33 and 23).  Few rows of up to 4096 vectors go to the
+// same workgroups of 512 threads (256 rows of 28000 columns 17 us, in 256
+// threads 23), many to smaller ones (800 rows: 38 us against 31).
+constexpr int kLongThreads = 512, kLongVecs = 8;
 RowPlan distill_plan(int64_t n, int64_t cols, int per_vec) {
   const int64_t vecs = (cols + per_vec - 1) / per_vec;
-  if (vecs > 4096 && vecs <= 16384 && n >= 128) return {1024, 16, static_cast<int>(cols), 1};
+  if (vecs > 512 && (vecs <= 4096 ? n < 512 : n >= 128)) return {kLongThreads, kLongVecs, static_cast<int>(cols), 1};
   return log_probs_plan(n, cols, per_vec);
 }
 
@@ -913,7 +1035,7 @@ hipError_t distill_typed(const DistillArgs& a, hipStream_t s) {
       if (p.vecs == 8) distill_tile_kernel<T, 256, 8, true><<<grid, 256, lds, s>>>(a, at, p.chunk, 1, stats);
       else distill_tile_kernel<T, 256, 16, true><<<grid, 256, lds, s>>>(a, at, p.chunk, 1, stats);
     } else {
-      distill_tile_kernel<T, 1024, 16, true><<<grid, 1024, lds, s>>>(a, at, p.chunk, 1, stats);
+      distill_long_kernel<T, kLongThreads, kLongVecs><<<grid, kLongThreads, lds, s>>>(a, at);
     }
   });
   if (e != hipSuccess || p.chunks == 1) return e;

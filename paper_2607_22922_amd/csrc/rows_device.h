@@ -15,6 +15,7 @@ typedef Word4 Word4At2 __attribute__((aligned(2)));
 __device__ __forceinline__ Word4 load_words(const void* p) {
   return __builtin_nontemporal_load(static_cast<const Word4At2*>(p));
 }
+__device__ __forceinline__ Word4 load_words_again(const void* p) { return *static_cast<const Word4At2*>(p); }
 __device__ __forceinline__ void store_words(void* p, Word4 w) {
   __builtin_nontemporal_store(w, static_cast<Word4At2*>(p));
 }
@@ -160,21 +161,36 @@ struct RowTile {
   float tail;
   int nvec, ntail;
 
+  // kOnce: nothing reads these bytes again soon (they pass the caches by).
+  template <bool kOnce = true>
   __device__ __forceinline__ void load(const T* x, int len) {
     const int tid = threadIdx.x;
     nvec = len / kE;
     ntail = len - nvec * kE;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      const int at = i * kThreads + tid;
+      // a scalar base and bound per round, one offset per thread
+      const char* from = reinterpret_cast<const char*>(x) + static_cast<int64_t>(i) * kThreads * 16;
       v[i] = Word4{Elem<T>::kNegInfWord, Elem<T>::kNegInfWord, Elem<T>::kNegInfWord, Elem<T>::kNegInfWord};
-      if (at < nvec) v[i] = load_words(reinterpret_cast<const char*>(x) + static_cast<uint32_t>(at) * 16u);
+      if (tid < nvec - i * kThreads) v[i] = kOnce ? load_words(from + tid * 16u) : load_words_again(from + tid * 16u);
     }
     tail = tid < ntail ? elem_load(x + nvec * kE + tid) : -INFINITY;
   }
   __device__ __forceinline__ bool has(int i) const { return i * kThreads < nvec; }
   __device__ __forceinline__ int column(int i, int j) const { return (i * kThreads + static_cast<int>(threadIdx.x)) * kE + j; }
   __device__ __forceinline__ int tail_column() const { return nvec * kE + static_cast<int>(threadIdx.x); }
+
+  // The thread's elements one by one from memory, for rare paths that must not
+  // cost the others registers: f(x, column).
+  template <typename F>
+  __device__ __forceinline__ void each_from_memory(const T* x, F&& f) const {
+#pragma unroll 1
+    for (int i = 0; i < kVecs; ++i)
+      if (static_cast<int>(threadIdx.x) < nvec - i * kThreads)
+#pragma unroll 1
+        for (int j = 0; j < kE; ++j) f(elem_load(x + column(i, j)), column(i, j));
+    if (static_cast<int>(threadIdx.x) < ntail) f(elem_load(x + tail_column()), tail_column());
+  }
 
   // Between two passes over the tile: the compiler would keep every unpacked
   // element of the first alive for the second (two to three times the registers).
