@@ -57,6 +57,13 @@ typedef int32_t ifvs_status;
 #define IFVS_MAX_CLAUSES 4
 #define IFVS_MAX_K       1024
 #define IFVS_MAX_ATTR    16
+#define IFVS_MAX_BAG     16       /* ids of one row of ifvs_embed_lookup                     */
+#define IFVS_MAX_TOP     32       /* alternatives of one row of ifvs_log_probs               */
+#define IFVS_MAX_COLS    (1 << 21) /* columns of a row of logits                             */
+
+#define IFVS_ELEM_F32  0          /* element types of the row operators                      */
+#define IFVS_ELEM_F16  1
+#define IFVS_ELEM_BF16 2
 
 typedef struct ifvs_index ifvs_index;   /* opaque; library-owned device state */
 
@@ -413,6 +420,39 @@ ifvs_status ifvs_train_step(ifvs_index* idx, int32_t nq, const float* q, const i
                             const float* w_z, const int32_t* cand, int32_t n_cand, int32_t n_pos, float tau,
                             float lambda, float lr, float* loss_out, float* dwz_out, void* stream);
 
+/* ifvs_score_candidates -- the student's scores of listed candidates:
+ *   logits_out[i][v] = -sum_{m<M} LUT_i[m][code of cand[i][v] in m]
+ * (ifvs_filtered_search's distance, negated), -inf for an absent candidate (an
+ * id outside 0..n-1, such as -1): rows of logits for ifvs_log_probs and
+ * ifvs_distill_loss.
+ *  lut: device [nq][m][256] in lut_dtype (from ifvs_build_lut)
+ *  cand: device [nq][n_cand] int32 original ids; logits_out: device
+ *        [nq][n_cand] fp32
+ * Enqueued on `stream`.  On a clustered index the first call allocates n ints.
+ * Errors: IFVS_E_STATE (NULL handle), IFVS_E_INVALID (nq, unknown dtype, n_cand
+ * outside 1..IFVS_MAX_COLS, NULL arrays), IFVS_E_NOMEM, IFVS_E_HIP. */
+ifvs_status ifvs_score_candidates(ifvs_index* idx, int32_t nq, const void* lut, int32_t lut_dtype,
+                                  const int32_t* cand, int32_t n_cand, float* logits_out, void* stream);
+
+/* ifvs_distill_step -- ifvs_train_step with the distillation loss in place of
+ * the labels' cross-entropy: the first n_teacher candidates of a query (its
+ * exact neighbours, say) come with the distances teacher_dist that a teacher
+ * gives them (ifvs_exact_search's), and the query's loss is
+ *   L_i = ifvs_distill_loss of the logits -d_v over the present candidates
+ *         against the teacher logits -teacher_dist[i][k] of slot k, temperature
+ *         tau (without teacher_lse; 0 where no teacher slot is present)
+ *         + lambda * mean over (m, c, j) of Delta_i[m][c][j]^2.
+ * Everything else, the arrays and their lifetimes included, is as in
+ * ifvs_train_step; teacher_dist: device [nq][n_teacher] fp32.  Besides the
+ * training workspace the first call, and a later one with more candidates than
+ * any before, allocates max_batch * (n_cand + 2 min(n_cand, 1024) + 1) words.
+ * Errors: as ifvs_train_step, plus IFVS_E_INVALID (n_teacher outside
+ * 1..min(n_cand, IFVS_MAX_K), NULL teacher_dist, 1 / tau not finite). */
+ifvs_status ifvs_distill_step(ifvs_index* idx, int32_t nq, const float* q, const ifvs_predicate* preds,
+                              const float* w_z, const int32_t* cand, int32_t n_cand, int32_t n_teacher,
+                              const float* teacher_dist, float tau, float lambda, float lr, float* loss_out,
+                              float* dwz_out, void* stream);
+
 /* ifvs_read_params -- copy the index's current memory bank ([bank_rows][m*r])
  * and W ([m][r][256][dim/m]) into caller memory (host or device; either
  * pointer may be NULL), enqueued on `stream`.
@@ -434,13 +474,6 @@ ifvs_status ifvs_read_params(const ifvs_index* idx, float* bank_out, float* W_ou
  * their first element at strides (`*_ld`, in elements) of at least the row's
  * length; columns are contiguous; no alignment beyond the element's is needed.
  * Sums are fp32 or fp64 in a fixed order: equal calls give equal bits. */
-#define IFVS_ELEM_F32  0
-#define IFVS_ELEM_F16  1
-#define IFVS_ELEM_BF16 2
-#define IFVS_MAX_BAG   16
-#define IFVS_MAX_TOP   32
-#define IFVS_MAX_COLS  (1 << 21)
-
 /* ifvs_embed_lookup -- out[i] = scale * sum over j < bag of table[ids[i][j]],
  * the sum in j order from +0 in fp32, one rounding to the element type at the
  * end.  An id outside 0..rows-1 (such as -1) is an absent slot; a row with no

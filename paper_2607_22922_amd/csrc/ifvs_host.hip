@@ -340,6 +340,12 @@ struct ifvs_index {
   float* tr_galpha = nullptr;    // [max_batch][m*r]
   int32_t* tr_rows = nullptr;    // [max_batch][h]
   int32_t* inv_perm = nullptr;   // original id -> physical row (clustered layouts)
+  // ifvs_distill_step's, sized by the most candidates of a call so far.
+  float* tr_logits = nullptr;    // [max_batch][tr_cand_cap]: scores, then their gradient
+  int32_t* tr_tids = nullptr;    // [max_batch][min(tr_cand_cap, 1024)]
+  float* tr_tlogits = nullptr;
+  float* tr_ce = nullptr;        // [max_batch]
+  int32_t tr_cand_cap = 0;
 
   // Every (n / kFences)-th clustered key, copied to the host at load: lets
   // the planner estimate each query's interval length without touching the
@@ -424,7 +430,8 @@ struct ifvs_index {
       if (p) hipFree(p);
     free_vectors();
     coarse.release();
-    for (void* p : {static_cast<void*>(tr_alpha), static_cast<void*>(tr_wf), static_cast<void*>(tr_lut),
+    for (void* p : {static_cast<void*>(tr_logits), static_cast<void*>(tr_tids), static_cast<void*>(tr_tlogits),
+                    static_cast<void*>(tr_ce), static_cast<void*>(tr_alpha), static_cast<void*>(tr_wf), static_cast<void*>(tr_lut),
                     static_cast<void*>(tr_gdelta), static_cast<void*>(tr_galpha), static_cast<void*>(tr_rows),
                     static_cast<void*>(inv_perm)})
       if (p) hipFree(p);
@@ -2467,17 +2474,84 @@ ifvs_status ifvs_probe_lds_gather(int32_t active_lanes, double* wave_reads_per_s
   return IFVS_OK;
 }
 
-ifvs_status ifvs_train_step(ifvs_index* idx, int32_t nq, const float* q, const ifvs_predicate* preds,
-                            const float* w_z, const int32_t* cand, int32_t n_cand, int32_t n_pos, float tau,
-                            float lambda, float lr, float* loss_out, float* dwz_out, void* stream) {
+namespace {
+
+// The workspace of the training calls, allocated by the first one.
+ifvs_status train_workspace(ifvs_index* idx) {
+  if (idx->tr_alpha) return IFVS_OK;
+  const int mr = idx->m * idx->r;
+  const size_t b = static_cast<size_t>(idx->max_batch);
+  ifvs_status st = IFVS_OK;
+  if ((st = dev_alloc(&idx->tr_alpha, b * mr, "training alpha")) != IFVS_OK ||
+      (st = dev_alloc(&idx->tr_wf, b * idx->dim, "training w_f")) != IFVS_OK ||
+      (st = dev_alloc(&idx->tr_lut, b * idx->m * kKsub, "training tables")) != IFVS_OK ||
+      (st = dev_alloc(&idx->tr_gdelta, b * idx->m * kKsub * idx->dsub, "training Delta gradients")) != IFVS_OK ||
+      (st = dev_alloc(&idx->tr_galpha, b * mr, "training alpha gradients")) != IFVS_OK ||
+      (st = dev_alloc(&idx->tr_rows, b * idx->h, "training bank rows")) != IFVS_OK) {
+    for (void* p : {static_cast<void*>(idx->tr_alpha), static_cast<void*>(idx->tr_wf),
+                    static_cast<void*>(idx->tr_lut), static_cast<void*>(idx->tr_gdelta),
+                    static_cast<void*>(idx->tr_galpha), static_cast<void*>(idx->tr_rows)})
+      if (p) hipFree(p);
+    idx->tr_alpha = idx->tr_wf = idx->tr_lut = idx->tr_gdelta = idx->tr_galpha = nullptr;
+    idx->tr_rows = nullptr;
+    return st;
+  }
+  return IFVS_OK;
+}
+
+// Scores, gradients and teachers of the distillation step, for n_cand
+// candidates a query: allocated by the first call, and anew by a call with
+// more candidates than any before (the free waits for the device).
+ifvs_status distill_buffers(ifvs_index* idx, int32_t n_cand) {
+  if (idx->tr_logits && idx->tr_cand_cap >= n_cand) return IFVS_OK;
+  for (void** p : {reinterpret_cast<void**>(&idx->tr_logits), reinterpret_cast<void**>(&idx->tr_tids),
+                   reinterpret_cast<void**>(&idx->tr_tlogits), reinterpret_cast<void**>(&idx->tr_ce)}) {
+    if (*p) (void)hipFree(*p);
+    *p = nullptr;
+  }
+  idx->tr_cand_cap = 0;
+  const size_t b = static_cast<size_t>(idx->max_batch);
+  const size_t teachers = b * std::min(n_cand, IFVS_MAX_K);
+  ifvs_status st = IFVS_OK;
+  if ((st = dev_alloc(&idx->tr_tids, teachers, "teacher slots")) != IFVS_OK ||
+      (st = dev_alloc(&idx->tr_tlogits, teachers, "teacher scores")) != IFVS_OK ||
+      (st = dev_alloc(&idx->tr_ce, b, "distillation losses")) != IFVS_OK ||
+      (st = dev_alloc(&idx->tr_logits, b * n_cand, "candidate scores")) != IFVS_OK)
+    return st;
+  idx->tr_cand_cap = n_cand;
+  return IFVS_OK;
+}
+
+// Candidates are original ids; the codes are in physical order.
+ifvs_status candidate_rows(ifvs_index* idx, hipStream_t s) {
+  if (!idx->perm || idx->inv_perm) return IFVS_OK;
+  if (ifvs_status st = dev_alloc(&idx->inv_perm, static_cast<size_t>(idx->n), "inverse permutation"); st != IFVS_OK)
+    return st;
+  if (hipError_t e = launch_invert_perm(idx->perm, idx->n, idx->inv_perm, s); e != hipSuccess) {
+    hipFree(idx->inv_perm);
+    idx->inv_perm = nullptr;
+    return hip_fail(e, "launching permutation inverse");
+  }
+  return IFVS_OK;
+}
+
+ifvs_status check_train(const ifvs_index* idx, int32_t nq, int32_t n_cand, float tau, float lambda, float lr) {
   if (ifvs_status st = check_index(idx); st != IFVS_OK) return st;
   if (ifvs_status st = check_nq(idx, nq); st != IFVS_OK) return st;
   if (idx->bank_rows == 0) return fail(IFVS_E_STATE, "the index has no memory bank and W to train");
   if (n_cand < 1 || n_cand > 4096) return fail(IFVS_E_INVALID, "n_cand must be in 1..4096");
-  if (n_pos < 0 || n_pos > n_cand) return fail(IFVS_E_INVALID, "n_pos must be in 0..n_cand");
   if (!(tau > 0.0f) || !std::isfinite(tau)) return fail(IFVS_E_INVALID, "tau must be positive and finite");
   if (!(lambda >= 0.0f) || !std::isfinite(lambda)) return fail(IFVS_E_INVALID, "lambda must be >= 0 and finite");
   if (!std::isfinite(lr)) return fail(IFVS_E_INVALID, "lr must be finite");
+  return IFVS_OK;
+}
+
+// One step.  teacher_dist null: the labels' cross-entropy (n_pos positives),
+// else the distillation loss against the first n_teacher candidates' distances.
+ifvs_status train_step(ifvs_index* idx, int32_t nq, const float* q, const ifvs_predicate* preds, const float* w_z,
+                       const int32_t* cand, int32_t n_cand, int32_t n_pos, int32_t n_teacher,
+                       const float* teacher_dist, float tau, float lambda, float lr, float* loss_out, float* dwz_out,
+                       void* stream) {
   if (nq == 0) return IFVS_OK;
   if (!q || !cand || !loss_out) return fail(IFVS_E_INVALID, "q, cand or loss_out is NULL");
   if (dwz_out && !w_z) return fail(IFVS_E_INVALID, "dwz_out needs w_z");
@@ -2486,34 +2560,10 @@ ifvs_status ifvs_train_step(ifvs_index* idx, int32_t nq, const float* q, const i
     return fail(IFVS_E_UNSUPPORTED, "one query's table, candidates and gradients exceed the 160 KB LDS budget");
   hipStream_t s = static_cast<hipStream_t>(stream);
   IFVS_HIP(hipSetDevice(idx->device), "hipSetDevice");
-  if (!idx->tr_alpha) {
-    const size_t b = static_cast<size_t>(idx->max_batch);
-    ifvs_status st = IFVS_OK;
-    if ((st = dev_alloc(&idx->tr_alpha, b * mr, "training alpha")) != IFVS_OK ||
-        (st = dev_alloc(&idx->tr_wf, b * idx->dim, "training w_f")) != IFVS_OK ||
-        (st = dev_alloc(&idx->tr_lut, b * idx->m * kKsub, "training tables")) != IFVS_OK ||
-        (st = dev_alloc(&idx->tr_gdelta, b * idx->m * kKsub * idx->dsub, "training Delta gradients")) != IFVS_OK ||
-        (st = dev_alloc(&idx->tr_galpha, b * mr, "training alpha gradients")) != IFVS_OK ||
-        (st = dev_alloc(&idx->tr_rows, b * idx->h, "training bank rows")) != IFVS_OK) {
-      for (void* p : {static_cast<void*>(idx->tr_alpha), static_cast<void*>(idx->tr_wf),
-                      static_cast<void*>(idx->tr_lut), static_cast<void*>(idx->tr_gdelta),
-                      static_cast<void*>(idx->tr_galpha), static_cast<void*>(idx->tr_rows)})
-        if (p) hipFree(p);
-      idx->tr_alpha = idx->tr_wf = idx->tr_lut = idx->tr_gdelta = idx->tr_galpha = nullptr;
-      idx->tr_rows = nullptr;
-      return st;
-    }
-  }
-  if (idx->perm && !idx->inv_perm) {
-    // Candidates are original ids; the codes are in physical order.
-    if (ifvs_status st = dev_alloc(&idx->inv_perm, static_cast<size_t>(idx->n), "inverse permutation"); st != IFVS_OK)
-      return st;
-    if (hipError_t e = launch_invert_perm(idx->perm, idx->n, idx->inv_perm, s); e != hipSuccess) {
-      hipFree(idx->inv_perm);
-      idx->inv_perm = nullptr;
-      return hip_fail(e, "launching permutation inverse");
-    }
-  }
+  if (ifvs_status st = train_workspace(idx); st != IFVS_OK) return st;
+  if (ifvs_status st = candidate_rows(idx, s); st != IFVS_OK) return st;
+  if (teacher_dist)
+    if (ifvs_status st = distill_buffers(idx, n_cand); st != IFVS_OK) return st;
   int slot = 0;
   if (ifvs_status st = stage_predicates(idx, nq, preds, false, false, s, &slot); st != IFVS_OK) return st;
   IFVS_LAUNCH(idx, kStCondition, s, "launching condition kernel",
@@ -2549,11 +2599,100 @@ ifvs_status ifvs_train_step(ifvs_index* idx, int32_t nq, const float* q, const i
   a.gdelta = idx->tr_gdelta;
   a.galpha = idx->tr_galpha;
   a.dwz = dwz_out;
+  if (teacher_dist) {
+    ScoreArgs c{};
+    c.codes_t = idx->codes_t;
+    c.inv_perm = idx->inv_perm;
+    c.n = idx->n;
+    c.m = idx->m;
+    c.mw = idx->mw;
+    c.lut = idx->tr_lut;
+    c.lut_dtype = IFVS_LUT_F32;
+    c.cand = cand;
+    c.nq = nq;
+    c.n_cand = n_cand;
+    c.logits = idx->tr_logits;
+    c.n_teacher = n_teacher;
+    c.teacher_dist = teacher_dist;
+    c.teacher_ids = idx->tr_tids;
+    c.teacher_logits = idx->tr_tlogits;
+    IFVS_HIP(launch_score_candidates(c, s), "launching candidate scores");
+    // Rows of at most 4096 candidates need no workspace; the gradient takes
+    // the logits' place.
+    DistillArgs d{};
+    d.n = nq;
+    d.cols = n_cand;
+    d.logits = idx->tr_logits;
+    d.ld = n_cand;
+    d.dtype = kElemF32;
+    d.n_teacher = n_teacher;
+    d.teacher_ids = idx->tr_tids;
+    d.teacher_logits = idx->tr_tlogits;
+    d.tau = tau;
+    d.c = 1.4426950408889634 / tau;
+    d.loss_out = idx->tr_ce;
+    d.grad_out = idx->tr_logits;
+    d.grad_ld = n_cand;
+    IFVS_HIP(launch_distill(d, s), "launching distillation loss");
+    a.glogit = idx->tr_logits;
+    a.ce = idx->tr_ce;
+  }
   IFVS_HIP(launch_train_query(a, s), "launching training gradient kernel");
   IFVS_HIP(launch_train_update_w(idx->W, idx->tr_gdelta, idx->tr_alpha, nq, idx->m, idx->r, idx->dsub, lr, s),
            "launching W update");
   IFVS_HIP(launch_train_update_bank(idx->bank, mr, idx->tr_rows, idx->h, idx->tr_galpha, nq, lr, s),
            "launching memory bank update");
+  return IFVS_OK;
+}
+
+}  // namespace
+
+ifvs_status ifvs_train_step(ifvs_index* idx, int32_t nq, const float* q, const ifvs_predicate* preds,
+                            const float* w_z, const int32_t* cand, int32_t n_cand, int32_t n_pos, float tau,
+                            float lambda, float lr, float* loss_out, float* dwz_out, void* stream) {
+  if (ifvs_status st = check_train(idx, nq, n_cand, tau, lambda, lr); st != IFVS_OK) return st;
+  if (n_pos < 0 || n_pos > n_cand) return fail(IFVS_E_INVALID, "n_pos must be in 0..n_cand");
+  return train_step(idx, nq, q, preds, w_z, cand, n_cand, n_pos, 0, nullptr, tau, lambda, lr, loss_out, dwz_out,
+                    stream);
+}
+
+ifvs_status ifvs_distill_step(ifvs_index* idx, int32_t nq, const float* q, const ifvs_predicate* preds,
+                              const float* w_z, const int32_t* cand, int32_t n_cand, int32_t n_teacher,
+                              const float* teacher_dist, float tau, float lambda, float lr, float* loss_out,
+                              float* dwz_out, void* stream) {
+  if (ifvs_status st = check_train(idx, nq, n_cand, tau, lambda, lr); st != IFVS_OK) return st;
+  if (n_teacher < 1 || n_teacher > std::min(n_cand, IFVS_MAX_K))
+    return fail(IFVS_E_INVALID, "n_teacher must be in 1..min(n_cand, 1024)");
+  if (!std::isfinite(1.4426950408889634f / tau)) return fail(IFVS_E_INVALID, "1 / tau must be finite");
+  if (nq > 0 && !teacher_dist) return fail(IFVS_E_INVALID, "teacher_dist is NULL");
+  return train_step(idx, nq, q, preds, w_z, cand, n_cand, 0, n_teacher, teacher_dist, tau, lambda, lr, loss_out,
+                    dwz_out, stream);
+}
+
+ifvs_status ifvs_score_candidates(ifvs_index* idx, int32_t nq, const void* lut, int32_t lut_dtype,
+                                  const int32_t* cand, int32_t n_cand, float* logits_out, void* stream) {
+  if (ifvs_status st = check_index(idx); st != IFVS_OK) return st;
+  if (ifvs_status st = check_nq(idx, nq); st != IFVS_OK) return st;
+  if (lut_dtype != IFVS_LUT_F32 && lut_dtype != IFVS_LUT_F16) return fail(IFVS_E_INVALID, "unknown lut_dtype");
+  if (n_cand < 1 || n_cand > IFVS_MAX_COLS) return fail(IFVS_E_INVALID, "n_cand must be in 1..2^21");
+  if (nq == 0) return IFVS_OK;
+  if (!lut || !cand || !logits_out) return fail(IFVS_E_INVALID, "lut, cand or logits_out is NULL");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  IFVS_HIP(hipSetDevice(idx->device), "hipSetDevice");
+  if (ifvs_status st = candidate_rows(idx, s); st != IFVS_OK) return st;
+  ScoreArgs a{};
+  a.codes_t = idx->codes_t;
+  a.inv_perm = idx->inv_perm;
+  a.n = idx->n;
+  a.m = idx->m;
+  a.mw = idx->mw;
+  a.lut = lut;
+  a.lut_dtype = lut_dtype;
+  a.cand = cand;
+  a.nq = nq;
+  a.n_cand = n_cand;
+  a.logits = logits_out;
+  IFVS_HIP(launch_score_candidates(a, s), "launching candidate scores");
   return IFVS_OK;
 }
 

@@ -170,6 +170,8 @@ struct TrainArgs {
   const int32_t* cand;       // [nq][n_cand] original ids (-1: absent), the first n_pos positives
   int nq, n_cand, n_pos;
   float tau, lam;
+  const float* glogit;       // [nq][n_cand] gradient of each query's loss by -distance (null: the labels' cross-entropy)
+  const float* ce;           // [nq] that loss (with glogit)
   int code_lds;              // set by the launcher: the candidates' code words are staged in LDS
   float* loss;               // [nq]
   float* gdelta;             // [nq][m][256][dsub]
@@ -177,6 +179,25 @@ struct TrainArgs {
   float* dwz;                // [nq][dim] or null
 };
 size_t train_query_lds_bytes(int m, int dim, int n_cand, int mr);
+// logits[q][v] = -distance of candidate v (-inf where absent); with
+// teacher_ids also, for the first n_teacher candidates, the slot itself (-1
+// where absent) and teacher_logits = -teacher_dist.
+struct ScoreArgs {
+  const uint32_t* codes_t;
+  const int32_t* inv_perm;   // null: identity
+  int64_t n;
+  int m, mw;
+  const void* lut;           // [nq][m][256]
+  int lut_dtype;
+  const int32_t* cand;       // [nq][n_cand]
+  int nq, n_cand;
+  float* logits;             // [nq][n_cand]
+  int n_teacher;
+  const float* teacher_dist; // [nq][n_teacher]
+  int32_t* teacher_ids;      // [nq][n_teacher] or null
+  float* teacher_logits;
+};
+hipError_t launch_score_candidates(const ScoreArgs& a, hipStream_t s);
 hipError_t launch_train_query(const TrainArgs& a, hipStream_t s);
 // W -= lr * sum_q gdelta_q (x) alpha_q, one thread per W entry.
 hipError_t launch_train_update_w(float* W, const float* gdelta, const float* alpha, int nq, int m, int r,

@@ -9,7 +9,8 @@
 // train_query_kernel (one workgroup per query):
 //   1. the query's table into LDS; its candidates' distances, summed over
 //      subspaces in order as the scan does;
-//   2. softmax statistics in fp64; g_v = d(batch loss)/d(distance of v);
+//   2. softmax statistics in fp64; g_v = d(batch loss)/d(distance of v); 1 and
+//      2 are skipped where the caller brings the gradient of another loss;
 //   3. the table gradient g_lut[m][c] = sum over candidates v whose code in
 //      subspace m is c of g_v, the candidates added in order by one
 //      wavefront (lane = subspace), in the table's LDS;
@@ -108,69 +109,80 @@ __global__ __launch_bounds__(kTrainThreads) void train_query_kernel(const TrainA
     return code_of(a, row, mm);
   };
 
-  // 1. Distances.
-  for (int v = tid; v < a.n_cand; v += kTrainThreads) {
-    const int64_t id = cand_id(a, qi, v);
-    float dist = 0.0f;
-    if (id >= 0) {
-      const int64_t row = a.code_lds ? 0 : (a.inv_perm ? a.inv_perm[id] : id);
-      for (int mm = 0; mm < M; ++mm) dist = __fadd_rn(dist, s_tab[mm * kKsub + code_at(v, row, mm)]);
+  double ce = 0.0;
+  if (a.glogit) {
+    // Another loss's gradient: d(batch loss)/d(distance) = -glogit / nq.
+    for (int v = tid; v < a.n_cand; v += kTrainThreads) {
+      const float g = a.glogit[static_cast<int64_t>(qi) * a.n_cand + v];
+      s_v[v] = cand_id(a, qi, v) >= 0 ? -g / static_cast<float>(a.nq) : 0.0f;
     }
-    s_v[v] = dist;
-  }
-  __syncthreads();
+    ce = static_cast<double>(a.ce[qi]);
+    __syncthreads();
+  } else {
+    // 1. Distances.
+    for (int v = tid; v < a.n_cand; v += kTrainThreads) {
+      const int64_t id = cand_id(a, qi, v);
+      float dist = 0.0f;
+      if (id >= 0) {
+        const int64_t row = a.code_lds ? 0 : (a.inv_perm ? a.inv_perm[id] : id);
+        for (int mm = 0; mm < M; ++mm) dist = __fadd_rn(dist, s_tab[mm * kKsub + code_at(v, row, mm)]);
+      }
+      s_v[v] = dist;
+    }
+    __syncthreads();
 
-  // 2. Softmax statistics over the present candidates (fp64).
-  const double inv_tau = 1.0 / static_cast<double>(a.tau);
-  double mx = -INFINITY, pos_sum = 0.0, n_p = 0.0;
-  for (int v = tid; v < a.n_cand; v += kTrainThreads) {
-    if (cand_id(a, qi, v) < 0) continue;
-    mx = fmax(mx, -static_cast<double>(s_v[v]) * inv_tau);
-    if (v < a.n_pos) {
-      pos_sum += static_cast<double>(s_v[v]);
-      n_p += 1.0;
+    // 2. Softmax statistics over the present candidates (fp64).
+    const double inv_tau = 1.0 / static_cast<double>(a.tau);
+    double mx = -INFINITY, pos_sum = 0.0, n_p = 0.0;
+    for (int v = tid; v < a.n_cand; v += kTrainThreads) {
+      if (cand_id(a, qi, v) < 0) continue;
+      mx = fmax(mx, -static_cast<double>(s_v[v]) * inv_tau);
+      if (v < a.n_pos) {
+        pos_sum += static_cast<double>(s_v[v]);
+        n_p += 1.0;
+      }
     }
-  }
-  mx = wave_max_d(mx);
-  pos_sum = wave_sum_d(pos_sum);
-  n_p = wave_sum_d(n_p);
-  if (lane == 0) {
-    s_red[wave] = mx;
-    s_red[kTrainWaves + wave] = pos_sum;
-    s_red[2 * kTrainWaves + wave] = n_p;
-  }
-  __syncthreads();
-  mx = s_red[0];
-  pos_sum = n_p = 0.0;
-#pragma unroll
-  for (int w = 0; w < kTrainWaves; ++w) {
-    mx = fmax(mx, s_red[w]);
-    pos_sum += s_red[kTrainWaves + w];
-    n_p += s_red[2 * kTrainWaves + w];
-  }
-  __syncthreads();
-  double z = 0.0;
-  for (int v = tid; v < a.n_cand; v += kTrainThreads)
-    if (cand_id(a, qi, v) >= 0) z += exp(-static_cast<double>(s_v[v]) * inv_tau - mx);
-  z = wave_sum_d(z);
-  if (lane == 0) s_red[wave] = z;
-  __syncthreads();
-  z = 0.0;
-#pragma unroll
-  for (int w = 0; w < kTrainWaves; ++w) z += s_red[w];
-  const double lse = mx + log(z);
-  const double ce = n_p > 0.0 ? lse + pos_sum * inv_tau / n_p : 0.0;
-  // g_v = -(softmax_v - [v positive] / P) / tau / nq (0 without positives).
-  for (int v = tid; v < a.n_cand; v += kTrainThreads) {
-    float g = 0.0f;
-    if (n_p > 0.0 && cand_id(a, qi, v) >= 0) {
-      const double p = exp(-static_cast<double>(s_v[v]) * inv_tau - lse);
-      const double share = v < a.n_pos ? 1.0 / n_p : 0.0;
-      g = static_cast<float>(-(p - share) * inv_tau / a.nq);
+    mx = wave_max_d(mx);
+    pos_sum = wave_sum_d(pos_sum);
+    n_p = wave_sum_d(n_p);
+    if (lane == 0) {
+      s_red[wave] = mx;
+      s_red[kTrainWaves + wave] = pos_sum;
+      s_red[2 * kTrainWaves + wave] = n_p;
     }
-    s_v[v] = g;
+    __syncthreads();
+    mx = s_red[0];
+    pos_sum = n_p = 0.0;
+#pragma unroll
+    for (int w = 0; w < kTrainWaves; ++w) {
+      mx = fmax(mx, s_red[w]);
+      pos_sum += s_red[kTrainWaves + w];
+      n_p += s_red[2 * kTrainWaves + w];
+    }
+    __syncthreads();
+    double z = 0.0;
+    for (int v = tid; v < a.n_cand; v += kTrainThreads)
+      if (cand_id(a, qi, v) >= 0) z += exp(-static_cast<double>(s_v[v]) * inv_tau - mx);
+    z = wave_sum_d(z);
+    if (lane == 0) s_red[wave] = z;
+    __syncthreads();
+    z = 0.0;
+#pragma unroll
+    for (int w = 0; w < kTrainWaves; ++w) z += s_red[w];
+    const double lse = mx + log(z);
+    ce = n_p > 0.0 ? lse + pos_sum * inv_tau / n_p : 0.0;
+    // g_v = -(softmax_v - [v positive] / P) / tau / nq (0 without positives).
+    for (int v = tid; v < a.n_cand; v += kTrainThreads) {
+      float g = 0.0f;
+      if (n_p > 0.0 && cand_id(a, qi, v) >= 0) {
+        const double p = exp(-static_cast<double>(s_v[v]) * inv_tau - lse);
+        const double share = v < a.n_pos ? 1.0 / n_p : 0.0;
+        g = static_cast<float>(-(p - share) * inv_tau / a.nq);
+      }
+      s_v[v] = g;
+    }
+    __syncthreads();
   }
-  __syncthreads();
 
   // 3. Table gradient: wavefront 0 adds the candidates in order, lane mm
   // updating subspace mm (one candidate touches one entry per subspace, and
@@ -371,6 +383,37 @@ __global__ __launch_bounds__(256) void train_update_bank_kernel(float* __restric
   }
 }
 
+// Scores of listed candidates (the Rank stage's distances, negated): a thread
+// per candidate, its table reads from the caches (a query's table is 16 to 120
+// KB and its candidates' workgroups read it together).
+constexpr int kScoreThreads = 256;
+template <typename L>
+__global__ __launch_bounds__(kScoreThreads) void score_candidates_kernel(const ScoreArgs a) {
+  const int qi = blockIdx.y;
+  const int v = blockIdx.x * kScoreThreads + threadIdx.x;
+  if (v >= a.n_cand) return;
+  const int64_t at = static_cast<int64_t>(qi) * a.n_cand + v;
+  const int64_t id = a.cand[at];
+  const bool there = id >= 0 && id < a.n;
+  float dist = 0.0f;
+  if (there) {
+    const int64_t row = a.inv_perm ? a.inv_perm[id] : id;
+    const uint32_t* words = a.codes_t + (row >> 6) * a.mw * 64 + (row & 63);
+    const L* lut = static_cast<const L*>(a.lut) + static_cast<int64_t>(qi) * a.m * kKsub;
+    for (int w = 0; w < a.mw; ++w) {
+      const uint32_t word = words[w * 64];
+      for (int b = 0; b < 4 && 4 * w + b < a.m; ++b)
+        dist = __fadd_rn(dist, static_cast<float>(lut[(4 * w + b) * kKsub + ((word >> (8 * b)) & 0xFFu)]));
+    }
+  }
+  a.logits[at] = there ? -dist : -INFINITY;
+  if (a.teacher_ids && v < a.n_teacher) {
+    const int64_t to = static_cast<int64_t>(qi) * a.n_teacher + v;
+    a.teacher_ids[to] = there ? v : -1;
+    a.teacher_logits[to] = -a.teacher_dist[to];
+  }
+}
+
 __global__ void invert_perm_kernel(const int32_t* __restrict__ perm, int64_t n, int32_t* __restrict__ inv) {
   const int64_t r = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
   if (r < n) inv[perm[r]] = static_cast<int32_t>(r);
@@ -413,6 +456,14 @@ hipError_t launch_train_update_bank(float* bank, int mr, const int32_t* rows, in
                                     int nq, float lr, hipStream_t s) {
   if (nq * h <= 0) return hipSuccess;
   train_update_bank_kernel<<<dim3(nq * h), dim3(256), 0, s>>>(bank, mr, rows, h, galpha, nq * h, lr);
+  return hipGetLastError();
+}
+
+hipError_t launch_score_candidates(const ScoreArgs& a, hipStream_t s) {
+  // grid.y counts to 65535, the most queries of a batch
+  const dim3 grid(static_cast<unsigned>((a.n_cand + kScoreThreads - 1) / kScoreThreads), static_cast<unsigned>(a.nq));
+  if (a.lut_dtype == 0) score_candidates_kernel<float><<<grid, kScoreThreads, 0, s>>>(a);
+  else score_candidates_kernel<_Float16><<<grid, kScoreThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 

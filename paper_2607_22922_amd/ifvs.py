@@ -44,7 +44,8 @@ EXPORTED = ("ifvs_load_index", "ifvs_free_index", "ifvs_select_codebook", "ifvs_
             "ifvs_build_coarse", "ifvs_lut_bounds", "ifvs_filtered_search_bounded", "ifvs_read_coarse",
             "ifvs_last_coarse", "ifvs_last_modes", "ifvs_query_batch",
             "ifvs_embed_lookup", "ifvs_embed_workspace", "ifvs_embed_gradient",
-            "ifvs_log_probs_workspace", "ifvs_log_probs", "ifvs_distill_workspace", "ifvs_distill_loss")
+            "ifvs_log_probs_workspace", "ifvs_log_probs", "ifvs_distill_workspace", "ifvs_distill_loss",
+            "ifvs_score_candidates", "ifvs_distill_step")
 
 
 class IfvsError(RuntimeError):
@@ -144,6 +145,8 @@ def _load_library() -> ctypes.CDLL:
         "ifvs_embed_gradient": ([i64, i32, i64, i32, vp, f32, vp, i64, i32, i32, vp, i64, i32, vp, i64, vp], i32),
         "ifvs_log_probs_workspace": ([i64, i64, i32], i64),
         "ifvs_log_probs": ([i64, i64, vp, i64, i32, vp, f32, vp, i32, i32, vp, vp, vp, vp, vp, i64, vp], i32),
+        "ifvs_score_candidates": ([vp, i32, vp, i32, vp, i32, vp, vp], i32),
+        "ifvs_distill_step": ([vp, i32, vp, vp, vp, vp, i32, i32, vp, f32, f32, f32, vp, vp, vp], i32),
         "ifvs_distill_workspace": ([i64, i64], i64),
         "ifvs_distill_loss": ([i64, i64, vp, i64, i32, vp, i32, vp, vp, vp, f32, vp, vp, vp, i64, vp, i64, vp],
                               i32),
@@ -439,6 +442,41 @@ class Index:
         dwz = torch.empty_like(q) if want_dwz else None
         self.train_step_into(q, pack_predicates(preds), None if w_z is None else w_z.contiguous(), cand, n_pos,
                              tau, lam, lr, loss, dwz)
+        return loss, dwz
+
+    def score_candidates_into(self, nq, lut, lut_dtype, cand, logits_out, stream=None):
+        """ifvs_score_candidates: -distance of each listed candidate."""
+        _check(_lib.ifvs_score_candidates(self.handle, nq, lut.data_ptr(), lut_dtype, cand.data_ptr(), cand.shape[1],
+                                          logits_out.data_ptr(), _stream(stream)))
+
+    def score_candidates(self, lut, cand, lut_dtype=LUT_F32):
+        """[nq][n_cand] logits of the candidates (ids, -1 absent) under the
+        tables, for log_probs and distill_loss."""
+        cand = cand.to(dtype=torch.int32).contiguous()
+        logits = torch.empty(cand.shape, device=self.device)
+        self.score_candidates_into(cand.shape[0], lut, lut_dtype, cand, logits)
+        return logits
+
+    def distill_step_into(self, q, preds_c, w_z, cand, teacher_dist, tau, lam, lr, loss_out, dwz_out=None,
+                          stream=None):
+        """One SGD step of the memory bank and W on the distillation loss (ifvs_distill_step)."""
+        _check(_lib.ifvs_distill_step(self.handle, q.shape[0], q.data_ptr(), preds_c, _ptr(w_z), cand.data_ptr(),
+                                      cand.shape[1], teacher_dist.shape[1], teacher_dist.data_ptr(), float(tau),
+                                      float(lam), float(lr), loss_out.data_ptr(), _ptr(dwz_out), _stream(stream)))
+
+    def distill_step(self, q, preds, w_z, cand, teacher_dist, tau, lam, lr, want_dwz=False):
+        """Marshalling wrapper: cand's first columns are the candidates whose
+        teacher distances teacher_dist [nq][n_teacher] holds.  Returns
+        (per-query loss, dL/dw_z or None)."""
+        q = q.contiguous()
+        cand = cand.to(dtype=torch.int32).contiguous()
+        teacher_dist = _dev_f32(teacher_dist, self.device)
+        if cand.shape[0] != q.shape[0] or teacher_dist.shape[0] != q.shape[0]:
+            raise IfvsError(E_INVALID, "q, cand and teacher_dist have different row counts")
+        loss = torch.empty(q.shape[0], device=self.device)
+        dwz = torch.empty_like(q) if want_dwz else None
+        self.distill_step_into(q, pack_predicates(preds), None if w_z is None else w_z.contiguous(), cand,
+                               teacher_dist, tau, lam, lr, loss, dwz)
         return loss, dwz
 
     def read_params(self):
