@@ -151,16 +151,24 @@ struct SortArgs {
   uint32_t* hist;      // [groups][1 << bits]
 };
 
-__device__ __forceinline__ void sort_entry(const SortArgs& a, bool first, int64_t at, uint32_t& key, uint32_t& from) {
-  if (first) {
-    const uint32_t id = static_cast<uint32_t>(a.ids[at]);
-    key = id < a.rows ? id : a.rows;
-    from = a.bag == 1 ? static_cast<uint32_t>(at) : static_cast<uint32_t>(at) / static_cast<uint32_t>(a.bag);
-  } else {
-    key = a.in.key[at];
-    from = a.in.from[at];
+// Where a pass reads its entries: the ids themselves, a buffer, or the LDS.
+struct FromIds {
+  const int32_t* ids;
+  uint32_t rows, bag;
+  __device__ __forceinline__ uint2 operator()(int64_t at) const {
+    const uint32_t slot = static_cast<uint32_t>(at);
+    return {min(static_cast<uint32_t>(ids[at]), rows), bag == 1 ? slot : slot / bag};
   }
-}
+};
+struct FromBuf {
+  SortBufs in;
+  __device__ __forceinline__ uint2 operator()(int64_t at) const { return {in.key[at], in.from[at]}; }
+};
+struct FromLds {
+  const uint2* list;
+  int64_t start;
+  __device__ __forceinline__ uint2 operator()(int64_t at) const { return list[at - start]; }
+};
 
 // Exclusive sum over 1024 threads.
 __device__ __forceinline__ uint32_t sort_scan(uint32_t v, uint32_t* s_wave) {
@@ -180,78 +188,78 @@ __device__ __forceinline__ uint32_t sort_scan(uint32_t v, uint32_t* s_wave) {
 }
 
 struct SortLds {
-  uint32_t count[kSortWaves][1 << kSortMaxBits];
+  uint16_t count[kSortWaves][1 << kSortMaxBits];     // of a tile: at most 4096
   uint32_t base[1 << kSortMaxBits];                  // where the digit's next entry goes
   uint32_t wave[kSortWaves];
 };
 
 // Counts of the digits of [lo, hi) into s.base.
-__device__ __forceinline__ void sort_count(const SortArgs& a, bool first, int64_t lo, int64_t hi, SortLds& s) {
+template <typename Src>
+__device__ __forceinline__ void sort_count(const SortArgs& a, const Src& src, int64_t lo, int64_t hi, SortLds& s) {
   const uint32_t mask = (1u << a.bits) - 1;
   s.base[threadIdx.x] = 0;
   __syncthreads();
-  for (int64_t at = lo + threadIdx.x; at < hi; at += kSortThreads) {
-    uint32_t key, from;
-    sort_entry(a, first, at, key, from);
-    atomicAdd(&s.base[(key >> a.shift) & mask], 1u);
-  }
+  for (int64_t at = lo + threadIdx.x; at < hi; at += kSortThreads)
+    atomicAdd(&s.base[(src(at).x >> a.shift) & mask], 1u);
   __syncthreads();
 }
 
 // Moves [lo, hi) to its places; s.base holds each digit's first one.
-__device__ __forceinline__ void sort_move(const SortArgs& a, bool first, int64_t lo, int64_t hi, SortLds& s) {
+template <typename Src>
+__device__ __forceinline__ void sort_move(const SortArgs& a, const Src& src, int64_t lo, int64_t hi, SortLds& s) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const uint32_t mask = (1u << a.bits) - 1;
+  const bool digit_thread = tid <= static_cast<int>(mask);
   for (int64_t tile = lo; tile < hi; tile += kSortTile) {
-    if (tid <= static_cast<int>(mask))
+    if (digit_thread)
 #pragma unroll
       for (int w = 0; w < kSortWaves; ++w) s.count[w][tid] = 0;
     __syncthreads();
-    uint32_t key[kSortRounds], from[kSortRounds], rank[kSortRounds];
+    const int64_t mine = tile + wave * kSortRounds * 64;
+    uint2 entry[kSortRounds];
+    uint32_t rank[kSortRounds];
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
-      const int64_t at = tile + (wave * kSortRounds + r) * 64 + lane;
-      key[r] = from[r] = 0;
-      if (at < hi) sort_entry(a, first, at, key[r], from[r]);
-    }
+    for (int r = 0; r < kSortRounds; ++r)
+      entry[r] = mine + r * 64 + lane < hi ? src(mine + r * 64 + lane) : uint2{0, 0};
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
-      const bool live = tile + (wave * kSortRounds + r) * 64 + lane < hi;
-      const uint32_t digit = (key[r] >> a.shift) & mask;
-      uint64_t peers = __ballot(live);
-      for (int b = 0; b < a.bits; ++b) {
-        const uint64_t set = __ballot((digit >> b) & 1u);
-        peers &= (digit >> b) & 1u ? set : ~set;
+    for (int r = 0; r < kSortRounds; ++r)
+      if (mine + r * 64 < hi) {
+        const bool live = mine + r * 64 + lane < hi;
+        const uint32_t digit = (entry[r].x >> a.shift) & mask;
+        uint64_t peers = __ballot(live);
+        for (int b = 0; b < a.bits; ++b) {
+          const uint64_t set = __ballot((digit >> b) & 1u);
+          peers &= (digit >> b) & 1u ? set : ~set;
+        }
+        const uint32_t before = s.count[wave][digit];
+        const int below = __popcll(peers & ((1ull << lane) - 1));
+        rank[r] = before + below;
+        group_sync<64>();
+        if (live && below == 0) s.count[wave][digit] = static_cast<uint16_t>(before + __popcll(peers));
+        group_sync<64>();
       }
-      const uint32_t before = s.count[wave][digit];
-      const int below = __popcll(peers & ((1ull << lane) - 1));
-      rank[r] = before + below;
-      group_sync<64>();
-      if (live && below == 0) s.count[wave][digit] = before + __popcll(peers);
-      group_sync<64>();
-    }
     __syncthreads();
-    // each wavefront's first place of digit `tid`
-    if (tid <= static_cast<int>(mask)) {
-      uint32_t next = s.base[tid];
+    // the tile's entries of digit `tid` before each wavefront's
+    uint32_t of_digit = 0;
+    if (digit_thread) {
 #pragma unroll
       for (int w = 0; w < kSortWaves; ++w) {
         const uint32_t n = s.count[w][tid];
-        s.count[w][tid] = next;
-        next += n;
+        s.count[w][tid] = static_cast<uint16_t>(of_digit);
+        of_digit += n;
       }
-      s.base[tid] = next;
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
-      if (tile + (wave * kSortRounds + r) * 64 + lane < hi) {
-        const uint32_t to = s.count[wave][(key[r] >> a.shift) & mask] + rank[r];
-        a.out.key[to] = key[r];
-        a.out.from[to] = from[r];
+    for (int r = 0; r < kSortRounds; ++r)
+      if (mine + r * 64 + lane < hi) {
+        const uint32_t digit = (entry[r].x >> a.shift) & mask;
+        const uint32_t to = s.base[digit] + s.count[wave][digit] + rank[r];
+        a.out.key[to] = entry[r].x;
+        a.out.from[to] = entry[r].y;
       }
-    }
     __syncthreads();
+    if (digit_thread) s.base[tid] += of_digit;
   }
 }
 
@@ -280,12 +288,13 @@ __device__ __forceinline__ void clear_rows(const ClearArgs& c, int64_t block) {
 __global__ __launch_bounds__(kSortThreads) void clear_kernel(const ClearArgs c) { clear_rows(c, blockIdx.x); }
 
 // Few slots, in one launch: every workgroup owns 1 << bits table rows, looks
-// through all ids for them (the L2 holds the ids), moves its slots, in order,
-// to where they lie in the whole order (it has counted the smaller ids on the
-// way), and sorts them there by one pass.  The owner of the last rows takes
+// through all ids for them (the L2 holds the ids), lists its slots in order (in
+// LDS, or where they lie in the whole order: it has counted the smaller ids on
+// the way), and sorts them by one pass.  The owner of the last rows takes
 // the absent slots.
 __global__ __launch_bounds__(kSortThreads) void sort_owned_kernel(const SortArgs a, const ClearArgs c) {
   __shared__ SortLds s;
+  __shared__ uint2 s_list[kSortTile];
   __shared__ uint32_t s_below[kSortWaves];
   if (static_cast<int>(blockIdx.x) >= a.groups) {
     clear_rows(c, blockIdx.x - a.groups);
@@ -335,26 +344,36 @@ __global__ __launch_bounds__(kSortThreads) void sort_owned_kernel(const SortArgs
     total += s.wave[w];
   }
   to += start;
+  if (total == 0) return;
+  const bool in_lds = total <= kSortTile;
   if (own > 0)
     each([&](int64_t at, bool live, uint32_t key) {
       const bool mine = live && key >= first && key < last;
       const uint64_t hits = __ballot(mine);
       if (mine) {
         const uint32_t p = to + __popcll(hits & ((1ull << lane) - 1));
-        a.in.key[p] = key;
-        a.in.from[p] = a.bag == 1 ? static_cast<uint32_t>(at) : static_cast<uint32_t>(at) / static_cast<uint32_t>(a.bag);
+        const uint32_t from = a.bag == 1 ? static_cast<uint32_t>(at) : static_cast<uint32_t>(at) / static_cast<uint32_t>(a.bag);
+        if (in_lds) {
+          s_list[p - start] = {key, from};
+        } else {
+          a.in.key[p] = key;
+          a.in.from[p] = from;
+        }
       }
       to += __popcll(hits);
     });
   __syncthreads();
-  sort_count(a, false, start, start + total, s);
-  const uint32_t n = s.base[tid];
-  if (total == 0) return;
-  __syncthreads();
-  const uint32_t base = sort_scan(n, s.wave);
-  s.base[tid] = start + base;
-  __syncthreads();
-  sort_move(a, false, start, start + total, s);
+  auto sort = [&](auto&& src) {
+    sort_count(a, src, start, start + total, s);
+    const uint32_t n = s.base[tid];
+    __syncthreads();
+    const uint32_t base = sort_scan(n, s.wave);
+    s.base[tid] = start + base;
+    __syncthreads();
+    sort_move(a, src, start, start + total, s);
+  };
+  if (in_lds) sort(FromLds{s_list, start});
+  else sort(FromBuf{a.in});
 }
 
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs a, int first, const ClearArgs c) {
@@ -364,7 +383,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs
     return;
   }
   const int64_t lo = blockIdx.x * a.per_group;
-  sort_count(a, first != 0, lo, min(a.slots, lo + a.per_group), s);
+  const int64_t hi = min(a.slots, lo + a.per_group);
+  if (first) sort_count(a, FromIds{a.ids, a.rows, static_cast<uint32_t>(a.bag)}, lo, hi, s);
+  else sort_count(a, FromBuf{a.in}, lo, hi, s);
   if (threadIdx.x < (1u << a.bits)) a.hist[(blockIdx.x << a.bits) + threadIdx.x] = s.base[threadIdx.x];
 }
 
@@ -388,16 +409,16 @@ __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(const SortArgs 
   s.base[tid] = base + before;
   __syncthreads();
   const int64_t lo = blockIdx.x * a.per_group;
-  sort_move(a, first != 0, lo, min(a.slots, lo + a.per_group), s);
+  const int64_t hi = min(a.slots, lo + a.per_group);
+  if (first) sort_move(a, FromIds{a.ids, a.rows, static_cast<uint32_t>(a.bag)}, lo, hi, s);
+  else sort_move(a, FromBuf{a.in}, lo, hi, s);
 }
 
 // ------------------------------------------------------------ summing runs
-// Sorted slots of a piece: about kPieces of them fill the GPU (512 slots: 10 ->
-// 4 us against pieces of 32), up to kLongPiece slots each (32768 slots, a row
-// of 13% of them: joining 19 us at 32, 11 at 64); kMaxPieces bounds the
-// longest join.
-constexpr int64_t kPieces = 512;
-constexpr int64_t kLongPiece = 64;
+// Sorted slots of a piece: about kPieces of them fill the GPU, up to kLongPiece
+// slots each; kMaxPieces bounds the longest join.
+constexpr int64_t kPieces = 1024;
+constexpr int64_t kLongPiece = 32;
 constexpr int64_t kMaxPieces = 1 << 13;
 constexpr int kAhead = 8;                  // gradient rows in flight per lane
 
@@ -498,64 +519,73 @@ __global__ __launch_bounds__(kEmbThreads) void embed_sum_kernel(const EmbedArgs 
   flush(hi < s.slots && s.key[hi] == run);
 }
 
-// A run that starts in a piece and goes on: its partial sums in order.  One
-// CU reads some 40 GB/s: a long run's columns go to workgroups of a wavefront
-// (2048 columns, 137 pieces: 26 -> 19 us).
-constexpr int kJoinThreads = 64;
+// A run that starts in a piece and goes on over `count` more: one workgroup per
+// piece and 64 vectors of columns (a CU reads some 40 GB/s, so a long run's
+// columns are spread).  Its four wavefronts each add a quarter of the partial
+// sums in order, and the quarters are added in order.
+constexpr int kJoinWaves = 4;
+constexpr uint32_t kJoinAhead = 8;              // partial sums in flight per lane
 template <typename T, typename O>
-__global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(const EmbedArgs a, const SumArgs s, int lanes,
-                                                                  int col_blocks) {
+__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(const EmbedArgs a, const SumArgs s,
+                                                                     int col_blocks) {
   constexpr int kE = Elem<T>::kPerVec;
-  const int lane = threadIdx.x & (lanes - 1);
-  const int groups = kJoinThreads / lanes;
-  const int64_t piece = static_cast<int64_t>(blockIdx.x) / col_blocks * groups + threadIdx.x / lanes;
-  const int vec = static_cast<int>(blockIdx.x % col_blocks) * kJoinThreads + lane;
-  if (piece >= s.pieces || vec * kE >= a.dim) return;
+  __shared__ float s_sum[kJoinWaves - 1][kE][64];
+  const int64_t piece = static_cast<int64_t>(blockIdx.x) / col_blocks;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t lo = piece * s.piece, hi = lo + s.piece;
   if (hi >= s.slots) return;
   const uint32_t run = s.key[hi - 1];
   if (run >= static_cast<uint32_t>(a.rows) || s.key[hi] != run) return;
   if (s.key[lo] == run && lo > 0 && s.key[lo - 1] == run) return;      // it started earlier
-  // Partial sums in order, kJoinAhead in flight; the keys that say whether the
-  // next ones belong to the run are read one step ahead of them.
-  constexpr uint32_t kJoinAhead = 16;
+  int64_t count = 0;
+  for (int64_t p = piece + 1;; p += 64 * kJoinWaves) {
+    const bool in = p + tid < s.pieces && s.key[(p + tid) * s.piece] == run;
+    const int n = __syncthreads_count(in ? 1 : 0);
+    count += n;
+    if (n < 64 * kJoinWaves) break;
+  }
+  const int vec = static_cast<int>(blockIdx.x % col_blocks) * 64 + lane;
+  const bool live = vec * kE < a.dim;
   float sum[kE];
-  {
-    const float* from = s.partial + (piece * 2 + 1) * s.pitch + vec * kE;
 #pragma unroll
-    for (int e = 0; e < kE; ++e) sum[e] = from[e];
-  }
-  // (No load waits for another: past the end both read the last piece's.)
-  auto look = [&](int64_t p0) {
-    uint32_t key[kJoinAhead], m = 0;
+  for (int e = 0; e < kE; ++e) sum[e] = 0.0f;
+  if (live) {
+    const int64_t p1 = piece + 1 + count * (wave + 1) / kJoinWaves;
+    int64_t p0 = piece + 1 + count * wave / kJoinWaves;
+    auto from = [&](int64_t p, int side) { return s.partial + (p * 2 + side) * s.pitch + vec * kE; };
+    if (wave == 0) {
+      const float* first = from(piece, 1);
 #pragma unroll
-    for (uint32_t u = 0; u < kJoinAhead; ++u) key[u] = s.key[min(p0 + u, s.pieces - 1) * s.piece];
+      for (int e = 0; e < kE; ++e) sum[e] = first[e];
+    }
+    for (; p0 < p1; p0 += kJoinAhead) {
+      float4 f[kJoinAhead][kE / 4];
 #pragma unroll
-    for (uint32_t u = 0; u < kJoinAhead; ++u) m += key[u] == run && p0 + u < s.pieces ? 1 : 0;
-    return m;
-  };
-  uint32_t mine = look(piece + 1);
-  for (int64_t p0 = piece + 1; mine != 0; p0 += kJoinAhead) {
-    float4 f[kJoinAhead][kE / 4];
+      for (uint32_t u = 0; u < kJoinAhead; ++u)
 #pragma unroll
-    for (uint32_t u = 0; u < kJoinAhead; ++u)
+        for (int e = 0; e < kE / 4; ++e) f[u][e] = *reinterpret_cast<const float4*>(from(min(p0 + u, p1 - 1), 0) + 4 * e);
 #pragma unroll
-      for (int e = 0; e < kE / 4; ++e)
-        f[u][e] = *reinterpret_cast<const float4*>(s.partial + min(p0 + u, s.pieces - 1) * 2 * s.pitch + vec * kE + 4 * e);
-    const uint32_t now = mine;
-    mine = now == kJoinAhead ? look(p0 + kJoinAhead) : 0;
+      for (uint32_t u = 0; u < kJoinAhead; ++u)
+        if (p0 + u < p1) {
 #pragma unroll
-    for (uint32_t u = 0; u < kJoinAhead; ++u)
-      if (u < now) {
-#pragma unroll
-        for (int e = 0; e < kE / 4; ++e) {
-          sum[4 * e] += f[u][e].x;
-          sum[4 * e + 1] += f[u][e].y;
-          sum[4 * e + 2] += f[u][e].z;
-          sum[4 * e + 3] += f[u][e].w;
+          for (int e = 0; e < kE / 4; ++e) {
+            sum[4 * e] += f[u][e].x;
+            sum[4 * e + 1] += f[u][e].y;
+            sum[4 * e + 2] += f[u][e].z;
+            sum[4 * e + 3] += f[u][e].w;
+          }
         }
-      }
+    }
   }
+  if (wave > 0)
+#pragma unroll
+    for (int e = 0; e < kE; ++e) s_sum[wave - 1][e][lane] = sum[e];
+  __syncthreads();
+  if (wave > 0 || !live) return;
+#pragma unroll
+  for (int w = 0; w < kJoinWaves - 1; ++w)
+#pragma unroll
+    for (int e = 0; e < kE; ++e) sum[e] += s_sum[w][e][lane];
   put_row<O>(a, LaneCols<T>(vec, a.dim), run, sum);
 }
 
@@ -704,10 +734,8 @@ hipError_t gradient_typed(const EmbedArgs& a, hipStream_t s) {
   embed_sum_kernel<T, O><<<static_cast<unsigned>((p.pieces + groups - 1) / groups * sum.col_blocks), kEmbThreads, 0,
                            s>>>(a, sum);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || p.pieces <= 1) return e;
-  const int lanes = std::min(sum.lanes, kJoinThreads), per = kJoinThreads / lanes;
-  const int col_blocks = (vecs + kJoinThreads - 1) / kJoinThreads;
-  embed_join_kernel<T, O><<<static_cast<unsigned>((p.pieces + per - 1) / per * col_blocks), kJoinThreads, 0, s>>>(
-      a, sum, lanes, col_blocks);
+  const int col_blocks = (vecs + 63) / 64;
+  embed_join_kernel<T, O><<<static_cast<unsigned>((p.pieces - 1) * col_blocks), 64 * kJoinWaves, 0, s>>>(a, sum, col_blocks);
   return hipGetLastError();
 }
 
