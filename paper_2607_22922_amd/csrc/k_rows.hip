@@ -187,33 +187,38 @@ __device__ __forceinline__ void best_columns(RowTile<T, kThreads, kVecs>& tile, 
   const float threshold = s.threshold;
   constexpr int kE = Elem<T>::kPerVec;
   if (thread_max >= threshold && thread_max > -INFINITY) {
-    auto keep = [&](float x, int column) {
-      if (x > -INFINITY) {
+    auto keep = [&](float f, int column) {
+      if (f >= threshold && f > -INFINITY) {
         const int at = atomicAdd(&s.count, 1);
-        if (at < kListCap) s.list[at] = column_key(x, first_column + column);
+        if (at < kListCap) s.list[at] = column_key(f, first_column + column);
       }
     };
     tile.forget_unpacked();
 #pragma unroll
     for (int i = 0; i < kVecs; ++i)
       if (tile.has(i)) {
-        // a vector's hits as a mask, walked only where there are any
+        // a vector's elements are looked at only where its maximum is enough
         float f[kE];
         Elem<T>::unpack(tile.v[i], f);
-        uint32_t hits = 0;
+        float most = f[0];
 #pragma unroll
-        for (int j = 0; j < kE; ++j) hits |= f[j] >= threshold ? 1u << j : 0u;
-        while (hits != 0) {
-          const int j = __builtin_ctz(hits);
-          hits &= hits - 1;
-          float y = f[0];
+        for (int j = 1; j < kE; ++j) most = fmaxf(most, f[j]);
+        if (most >= threshold) {
+          uint32_t hits = 0;
 #pragma unroll
-          for (int o = 1; o < kE; ++o) y = j == o ? f[o] : y;
-          keep(y, tile.column(i, j));
+          for (int j = 0; j < kE; ++j) hits |= f[j] >= threshold ? 1u << j : 0u;
+          while (hits != 0) {
+            const int j = __builtin_ctz(hits);
+            hits &= hits - 1;
+            float y = f[0];
+#pragma unroll
+            for (int o = 1; o < kE; ++o) y = j == o ? f[o] : y;
+            keep(y, tile.column(i, j));
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-    if (tile.tail >= threshold) keep(tile.tail, tile.tail_column());
+    keep(tile.tail, tile.tail_column());
   }
   group_sync<kThreads>();
   const int m = s.count;
