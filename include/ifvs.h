@@ -473,7 +473,8 @@ ifvs_status ifvs_read_params(const ifvs_index* idx, float* bank_out, float* W_ou
  * graphs replayed side by side) need a workspace each.  Rows are counted from
  * their first element at strides (`*_ld`, in elements) of at least the row's
  * length; columns are contiguous; no alignment beyond the element's is needed.
- * Sums are fp32 or fp64 in a fixed order: equal calls give equal bits. */
+ * Sums are fp32 or fp64 in an order fixed by sizes and alignment: equal calls
+ * give equal bits. */
 /* ifvs_embed_lookup -- out[i] = scale * sum over j < bag of table[ids[i][j]],
  * the sum in j order from +0 in fp32, one rounding to the element type at the
  * end.  An id outside 0..rows-1 (such as -1) is an absent slot; a row with no

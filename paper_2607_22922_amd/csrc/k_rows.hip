@@ -101,7 +101,7 @@ __device__ __forceinline__ Stat wave_stat(RowTile<T, kThreads, kVecs>& tile, con
         for (int j = 0; j < kE; ++j) add(f[j]);
         __builtin_amdgcn_sched_barrier(0);
       }
-    add(tile.tail);
+    add(tile.edge);
   } else {
     origin = static_cast<double>(mx) * c;
     tile.each_from_memory(x, [&](float v, int) { sum += v == mx ? 1.0f : (isnan(v) ? NAN : 0.0f); });
@@ -218,7 +218,7 @@ __device__ __forceinline__ void best_columns(RowTile<T, kThreads, kVecs>& tile, 
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-    keep(tile.tail, tile.tail_column());
+    keep(tile.edge, tile.edge_column());
   }
   group_sync<kThreads>();
   const int m = s.count;
@@ -594,11 +594,12 @@ __device__ __forceinline__ Stat other_stat(RowTile<T, kThreads, kVecs>& tile, co
         for (int j = 0; j < kE; ++j) add(f[j]);
         __builtin_amdgcn_sched_barrier(0);
       }
-    add(tile.tail);
+    add(tile.edge);
   } else {
     origin = mx * a.c;
     tile.each_from_memory(x, [&](float v, int column) {
-      if ((bits[column / kE] >> (column % kE)) & 1u) return;
+      const int bit = tile.bit_of(column);
+      if ((bits[bit >> 3] >> (bit & 7)) & 1u) return;
       sum += v == mx ? 1.0f : (isnan(v) ? NAN : 0.0f);
     });
     if (mx == INFINITY) sum = NAN;
@@ -614,9 +615,9 @@ __device__ __forceinline__ void fill_range(T* p, int n, float g, int tid, int th
 #pragma unroll
   for (int j = 0; j < kE; ++j) f[j] = g;
   const Word4 w = Elem<T>::pack(f);
-  const int nvec = n / kE;
-  for (int v = tid; v < nvec; v += threads) store_words(p + v * kE, w);
-  for (int v = nvec * kE + tid; v < n; v += threads) p[v] = elem_round<T>(g);
+  const int head = head_of(p, max(n, 0)), nvec = (n - head) / kE;
+  for (int v = tid; v < nvec; v += threads) store_words(p + head + v * kE, w);
+  if (tid < n - nvec * kE) p[tid < head ? tid : nvec * kE + tid] = elem_round<T>(g);
 }
 
 // The gradient of the tile's columns, every one as an other one.
@@ -642,12 +643,12 @@ __device__ __forceinline__ void write_others(RowTile<T, kThreads, kVecs>& tile, 
         Elem<T>::unpack(tile.v[i], f);
 #pragma unroll
         for (int j = 0; j < kE; ++j) f[j] = gradient(f[j]);
-        char* to = reinterpret_cast<char*>(grad) + static_cast<int64_t>(i) * kThreads * 16;
+        char* to = reinterpret_cast<char*>(grad + tile.head) + static_cast<int64_t>(i) * kThreads * 16;
         store_words(to + tid * 16u, Elem<T>::pack(f));
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-  if (tid < tile.ntail) grad[tile.tail_column()] = elem_round<T>(gradient(tile.tail));
+  if (tid < tile.nedge) grad[tile.edge_column()] = elem_round<T>(gradient(tile.edge));
 }
 
 // After the tile: the loss, and the named columns' gradient over what
@@ -701,16 +702,17 @@ __device__ __forceinline__ void gather_named(const DistillArgs& a, const T* x, c
 
 // A bit for every named column of [first, first + columns), by one wavefront.
 template <typename T, int kThreads, int kVecs>
-__device__ __forceinline__ void mark_named(const DistillArgs& a, const TeacherLds& t, int first, int columns) {
-  constexpr int kBitWords = (kThreads * kVecs + 16) / 16;
+__device__ __forceinline__ void mark_named(const RowTile<T, kThreads, kVecs>& tile, const DistillArgs& a,
+                                           const TeacherLds& t, int first, int columns) {
+  constexpr int kBitWords = (RowTile<T, kThreads, kVecs>::kBitBytes + 15) / 16;
   const int lane = threadIdx.x & 63;
   for (int w = lane; w < kBitWords; w += 64) reinterpret_cast<Word4*>(t.bits)[w] = Word4{0, 0, 0, 0};
   group_sync<64>();
   for (int k = lane; k < a.n_teacher; k += 64) {
     const int column = t.column[k] - first;
     if (t.column[k] >= 0 && column >= 0 && column < columns) {
-      const int vec = column / Elem<T>::kPerVec;
-      atomicOr(reinterpret_cast<unsigned*>(t.bits) + (vec >> 2), 1u << (8 * (vec & 3) + column % Elem<T>::kPerVec));
+      const int bit = tile.bit_of(column);
+      atomicOr(reinterpret_cast<unsigned*>(t.bits) + (bit >> 5), 1u << (bit & 31));
     }
   }
 }
@@ -732,7 +734,7 @@ __device__ __forceinline__ void drop_named(RowTile<T, kThreads, kVecs>& tile, co
         tile.v[i] = Elem<T>::pack(f);
       }
     }
-  if (tid < tile.ntail && ((bits[tile.nvec] >> tid) & 1u)) tile.tail = -INFINITY;
+  if (tid < tile.nedge && ((bits[kThreads * kVecs + (tid >> 3)] >> (tid & 7)) & 1u)) tile.edge = -INFINITY;
 }
 
 // What the wavefront that reads the teacher leaves for the workgroup.
@@ -805,10 +807,11 @@ __global__ __launch_bounds__(kThreads, 4) void distill_tile_kernel(const Distill
   // The teacher's wavefront has no registers for its mathematics beside a
   // large tile: it reads its part of the row afterwards.
   constexpr bool kTeacherFirst = kVecs > 8;
+  tile.place(x, mine);
   if (!kTeacherFirst) tile.load(x, mine);
   if (tid < 64) {
     teacher_state<T, kThreads, kVecs>(a, row, x, len, first, mine, t, s_teacher);
-    mark_named<T, kThreads, kVecs>(a, t, 0, mine);
+    mark_named(tile, a, t, 0, mine);
   }
   if (kTeacherFirst) tile.load(x, mine);
   group_sync<kThreads>();
@@ -857,7 +860,7 @@ __global__ __launch_bounds__(kThreads) void distill_long_kernel(const DistillArg
     const int n = min(mine - at, Tile::kCapacity);
     if (at > 0 && grad) tile.template load<false>(x + at, n);
     else tile.load(x + at, n);
-    if (tid < 64) mark_named<T, kThreads, kVecs>(a, t, at, n);
+    if (tid < 64) mark_named(tile, a, t, at, n);
     __syncthreads();
     drop_named(tile, t.bits);
     other = join(other, other_stat(tile, x + at, t.bits, wave_max(tile.thread_max()), a));
@@ -1027,7 +1030,7 @@ hipError_t distill_typed(const DistillArgs& a, hipStream_t s) {
   const RowPlan p = distill_plan(a.n, a.cols, Elem<T>::kPerVec);
   DistillStat* stats = static_cast<DistillStat*>(a.workspace);
   const size_t slots = static_cast<size_t>(a.n_teacher) * 16 + 8;
-  const size_t lds = ((slots + 15) & ~size_t{15}) + static_cast<size_t>(p.threads) * p.vecs + 16;
+  const size_t lds = ((slots + 15) & ~size_t{15}) + static_cast<size_t>(p.threads) * p.vecs + 32;
   const int64_t items = a.n * p.chunks;
   const hipError_t e = in_slices(items, [&](int64_t at, unsigned grid) {
     if (p.chunks > 1) {

@@ -149,36 +149,63 @@ __device__ __forceinline__ void group_sync() {
   }
 }
 
-// Up to kThreads * kVecs vectors and a tail of less than one vector of a row,
-// in the registers of a workgroup: thread t holds vectors t, t + kThreads, ...
-// and element t of the tail; places past the end hold -inf.  Loops step over
-// vector rounds that lie wholly past the end.
+// Elements before the first 16-byte boundary at or after p, at most len.
+template <typename T>
+__device__ __forceinline__ int head_of(const T* p, int len) {
+  const int off = static_cast<int>(reinterpret_cast<uintptr_t>(p) & 15);
+  return min(len, ((16 - off) & 15) / static_cast<int>(sizeof(T)));
+}
+
+// Up to kThreads * kVecs aligned vectors of a row, and its edges (less than a
+// vector before the first and after the last), in the registers of a
+// workgroup: thread t holds vectors t, t + kThreads, ... and edge element t;
+// places past the end hold -inf.  (Vectors that straddle cache lines cost a
+// fifth: 2048 rows of 50001 fp16 logits 47 us unaligned, of 50048 39.)  Loops
+// step over vector rounds that lie wholly past the end.
 template <typename T, int kThreads, int kVecs>
 struct RowTile {
   static constexpr int kE = Elem<T>::kPerVec;
   static constexpr int kCapacity = kThreads * kVecs * kE;
   Word4 v[kVecs];
-  float tail;
-  int nvec, ntail;
+  float edge;
+  int head, nvec, nedge;       // elements before the first vector, vectors, edge elements
 
+  // The layout of len elements at x, without reading them.
+  __device__ __forceinline__ void place(const T* x, int len) {
+    head = head_of(x, len);
+    nvec = (len - head) / kE;
+    nedge = len - nvec * kE;
+  }
   // kOnce: nothing reads these bytes again soon (they pass the caches by).
   template <bool kOnce = true>
   __device__ __forceinline__ void load(const T* x, int len) {
     const int tid = threadIdx.x;
-    nvec = len / kE;
-    ntail = len - nvec * kE;
+    place(x, len);
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
       // a scalar base and bound per round, one offset per thread
-      const char* from = reinterpret_cast<const char*>(x) + static_cast<int64_t>(i) * kThreads * 16;
+      const char* from = reinterpret_cast<const char*>(x + head) + static_cast<int64_t>(i) * kThreads * 16;
       v[i] = Word4{Elem<T>::kNegInfWord, Elem<T>::kNegInfWord, Elem<T>::kNegInfWord, Elem<T>::kNegInfWord};
       if (tid < nvec - i * kThreads) v[i] = kOnce ? load_words(from + tid * 16u) : load_words_again(from + tid * 16u);
     }
-    tail = tid < ntail ? elem_load(x + nvec * kE + tid) : -INFINITY;
+    edge = tid < nedge ? elem_load(x + edge_column()) : -INFINITY;
   }
   __device__ __forceinline__ bool has(int i) const { return i * kThreads < nvec; }
-  __device__ __forceinline__ int column(int i, int j) const { return (i * kThreads + static_cast<int>(threadIdx.x)) * kE + j; }
-  __device__ __forceinline__ int tail_column() const { return nvec * kE + static_cast<int>(threadIdx.x); }
+  __device__ __forceinline__ int column(int i, int j) const {
+    return head + (i * kThreads + static_cast<int>(threadIdx.x)) * kE + j;
+  }
+  __device__ __forceinline__ int edge_column() const {
+    const int tid = threadIdx.x;
+    return tid < head ? tid : nvec * kE + tid;
+  }
+  // A bit per column: byte and bit of a column; the edges' two bytes follow
+  // the vectors'.
+  static constexpr int kBitBytes = kThreads * kVecs + 2;
+  __device__ __forceinline__ int bit_of(int column) const {
+    const int in = column - head;
+    if (in >= 0 && in < nvec * kE) return in / kE * 8 + in % kE;
+    return kThreads * kVecs * 8 + (in < 0 ? column : column - nvec * kE);
+  }
 
   // The thread's elements one by one from memory, for rare paths that must not
   // cost the others registers: f(x, column).
@@ -189,7 +216,7 @@ struct RowTile {
       if (static_cast<int>(threadIdx.x) < nvec - i * kThreads)
 #pragma unroll 1
         for (int j = 0; j < kE; ++j) f(elem_load(x + column(i, j)), column(i, j));
-    if (static_cast<int>(threadIdx.x) < ntail) f(elem_load(x + tail_column()), tail_column());
+    if (static_cast<int>(threadIdx.x) < nedge) f(elem_load(x + edge_column()), edge_column());
   }
 
   // Between two passes over the tile: the compiler would keep every unpacked
@@ -201,7 +228,7 @@ struct RowTile {
 
   // Maximum of the thread's elements (NaN ones are passed over).
   __device__ __forceinline__ float thread_max() const {
-    float m = tail;
+    float m = edge;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i)
       if (has(i)) {
