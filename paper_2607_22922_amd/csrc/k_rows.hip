@@ -111,17 +111,23 @@ __device__ __forceinline__ Stat wave_stat(RowTile<T, kThreads, kVecs>& tile, con
 }
 
 // ------------------------------------------------------------ best columns
+// Whole numbers in the order of the logits (+0 and -0 equal).
+__device__ __forceinline__ uint32_t ordered_bits(float v) {
+  const uint32_t b = __float_as_uint(v + 0.0f);
+  return (b >> 31) ? ~b : (b | 0x80000000u);
+}
+__device__ __forceinline__ float from_ordered(uint32_t o) {
+  return __uint_as_float((o >> 31) ? (o & 0x7FFFFFFFu) : ~o);
+}
+
 // A column as a whole number: larger is better, ties to the lower column; 0 is
-// none.  +0 and -0 are equal.
+// none.
 __device__ __forceinline__ uint64_t column_key(float x, int column) {
-  const uint32_t b = __float_as_uint(x + 0.0f);
-  const uint32_t ordered = (b >> 31) ? ~b : (b | 0x80000000u);
-  return (static_cast<uint64_t>(ordered) << 32) | static_cast<uint32_t>(~column);
+  return (static_cast<uint64_t>(ordered_bits(x)) << 32) | static_cast<uint32_t>(~column);
 }
 __device__ __forceinline__ int key_column(uint64_t key) { return static_cast<int>(~static_cast<uint32_t>(key)); }
 __device__ __forceinline__ float key_logit(uint64_t key) {
-  const uint32_t o = static_cast<uint32_t>(key >> 32);
-  return __uint_as_float((o >> 31) ? (o & 0x7FFFFFFFu) : ~o);
+  return from_ordered(static_cast<uint32_t>(key >> 32));
 }
 
 template <int kCtrl>
@@ -144,20 +150,30 @@ __device__ __forceinline__ uint64_t wave_key_max(uint64_t v) {
   return key_max(key_max(key_lane(v, 0), key_lane(v, 16)), key_max(key_lane(v, 32), key_lane(v, 48)));
 }
 
-// The nth largest (1-based) of a wavefront's 64 values.
-__device__ __forceinline__ float nth_largest(float v, int nth) {
-  int greater = 0;
+// A value that at least nth of a wavefront's 64 values reach: the nth largest,
+// rounded down to bf16.  A bisection over its 16 leading bits, a comparison and
+// a count of lanes each (64 comparisons with every lane's value cost three
+// times the vector instructions).
+__device__ __forceinline__ float reached_by(float v, int nth) {
+  const uint32_t key = ordered_bits(v);
+  uint32_t cut = 0;
 #pragma unroll
-  for (int s = 0; s < 64; ++s) greater += lane_of(v, s) > v ? 1 : 0;
-  return -wave_max(greater < nth ? -v : -INFINITY);
+  for (int b = 31; b >= 16; --b) {
+    const uint32_t t = cut | (1u << b);
+    if (__popcll(__ballot(key >= t)) >= nth) cut = t;
+  }
+  // below the keys of all numbers: everything reaches it
+  return cut <= ordered_bits(-INFINITY) ? -INFINITY : from_ordered(cut);
 }
 
 // Shared memory of best_columns.
+constexpr int kStaged = 8;                 // threads whose elements a wavefront lays out
+template <int kThreads, int kVecs>
 struct BestLds {
+  Word4 stage[kThreads / 64][kStaged][kVecs];
   uint64_t list[kListCap];
-  uint64_t round[16];
+  uint64_t round[kThreads / 64];
   float group[kGroups];
-  float threshold;
   int count;
 };
 
@@ -165,12 +181,19 @@ struct BestLds {
 // order, 0 past the last: emit(rank, key) once per rank, by some thread.
 // Every element at least as large as the n_top-th largest of the 64 group
 // maxima is collected (n_top of them at least, few more unless the row is
-// full of ties) and ranked by counting.  More than the list holds: one round
-// over the tile's len elements at x per rank.
+// full of ties) and ranked by counting.  Few threads hold such an element: they
+// lay their vectors out in LDS and their wavefront looks at them an element a
+// lane (2048 rows of 50001 fp16 logits, 10 alternatives: 48 us, each thread
+// looking at its own 54), except that where many lanes of a single wavefront
+// hold one each looks at its own (4096 rows of 1000, 32 alternatives: 11 us
+// against 18).  More than the list holds: one round over the
+// tile's len elements at x per rank.
 template <typename T, int kThreads, int kVecs, typename Emit>
 __device__ __forceinline__ void best_columns(RowTile<T, kThreads, kVecs>& tile, float thread_max,
-                                             const T* x, int len, int first_column, int n_top, BestLds& s, Emit emit) {
-  const int tid = threadIdx.x;
+                                             const T* x, int len, int first_column, int n_top,
+                                             BestLds<kThreads, kVecs>& s, Emit emit) {
+  constexpr int kE = Elem<T>::kPerVec;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   constexpr int kPer = kThreads / kGroups;
   float g = thread_max;
   if constexpr (kPer == 4) g = quad_max(g);
@@ -179,21 +202,37 @@ __device__ __forceinline__ void best_columns(RowTile<T, kThreads, kVecs>& tile, 
   if (tid % kPer == 0) s.group[tid / kPer] = g;
   if (tid == 0) s.count = 0;
   group_sync<kThreads>();
-  if (tid < 64) {
-    const float t = nth_largest(s.group[tid], n_top);
-    if (tid == 0) s.threshold = t;
-  }
-  group_sync<kThreads>();
-  const float threshold = s.threshold;
-  constexpr int kE = Elem<T>::kPerVec;
-  if (thread_max >= threshold && thread_max > -INFINITY) {
-    auto keep = [&](float f, int column) {
-      if (f >= threshold && f > -INFINITY) {
-        const int at = atomicAdd(&s.count, 1);
-        if (at < kListCap) s.list[at] = column_key(f, first_column + column);
+  const float threshold = reached_by(s.group[lane], n_top);
+  auto keep = [&](float f, int column) {
+    if (f >= threshold && f > -INFINITY) {
+      const int at = atomicAdd(&s.count, 1);
+      if (at < kListCap) s.list[at] = column_key(f, first_column + column);
+    }
+  };
+  keep(tile.edge, tile.edge_column());
+  uint64_t holders = __ballot(thread_max >= threshold && thread_max > -INFINITY);
+  tile.forget_unpacked();
+  if (kThreads > 64 || __popcll(holders) <= kStaged) {
+    while (holders != 0) {
+      const int mine = __popcll(holders & ((1ull << lane) - 1));
+      if (((holders >> lane) & 1u) && mine < kStaged) {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) s.stage[wave][mine][i] = tile.v[i];
       }
-    };
-    tile.forget_unpacked();
+      group_sync<64>();
+      for (int h = 0; h < kStaged && holders != 0; ++h, holders &= holders - 1) {
+        const int owner = (tid & ~63) + __builtin_ctzll(holders);
+        const T* staged = reinterpret_cast<const T*>(&s.stage[wave][h][0]);
+#pragma unroll
+        for (int e0 = 0; e0 < kVecs * kE; e0 += 64) {
+          const int e = e0 + lane;
+          if (kVecs * kE >= 64 || e < kVecs * kE)
+            keep(static_cast<float>(staged[e]), tile.head + (e / kE * kThreads + owner) * kE + e % kE);
+        }
+      }
+      group_sync<64>();
+    }
+  } else if ((holders >> lane) & 1u) {
 #pragma unroll
     for (int i = 0; i < kVecs; ++i)
       if (tile.has(i)) {
@@ -218,7 +257,6 @@ __device__ __forceinline__ void best_columns(RowTile<T, kThreads, kVecs>& tile, 
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-    keep(tile.edge, tile.edge_column());
   }
   group_sync<kThreads>();
   const int m = s.count;
@@ -292,7 +330,7 @@ template <typename T, int kThreads, int kVecs, bool kWhole>
 __global__ __launch_bounds__(kThreads, 4) void log_probs_tile_kernel(const LogProbArgs a, int64_t item0, int chunk,
                                                                      int chunks, Stat* stats, uint64_t* keys) {
   constexpr int kWaves = kThreads / 64;
-  __shared__ BestLds s_best;
+  __shared__ BestLds<kThreads, kVecs> s_best;
   __shared__ Stat s_stat[kWaves];
   const int tid = threadIdx.x, wave = tid >> 6;
   const int64_t item = item0 + blockIdx.x;
