@@ -59,7 +59,7 @@ typedef int32_t ifvs_status;
 #define IFVS_MAX_ATTR    16
 #define IFVS_MAX_BAG     16       /* ids of one row of ifvs_embed_lookup                     */
 #define IFVS_MAX_TOP     32       /* alternatives of one row of ifvs_log_probs               */
-#define IFVS_MAX_COLS    (1 << 21) /* columns of a row of logits                             */
+#define IFVS_MAX_COLS    (1 << 20) /* columns of a row of logits                             */
 
 #define IFVS_ELEM_F32  0          /* element types of the row operators                      */
 #define IFVS_ELEM_F16  1
@@ -484,7 +484,7 @@ ifvs_status ifvs_read_params(const ifvs_index* idx, float* bank_out, float* W_ou
  *  out:   device [n] rows of dim elements of type dtype, out_ld apart; must
  *         not overlap the table
  * Enqueued on `stream`; n = 0 writes nothing.
- * Errors: IFVS_E_INVALID (rows outside 1..2^31-2, dim outside 1..2^20, bag
+ * Errors: IFVS_E_INVALID (rows outside 1..2^31-2, dim outside 1..65536, bag
  * outside 1..IFVS_MAX_BAG, n * bag outside 0..2^30, a stride below dim,
  * non-finite scale, unknown dtype, NULL or misaligned arrays), IFVS_E_HIP. */
 ifvs_status ifvs_embed_lookup(int64_t rows, int32_t dim, const void* table, int64_t table_ld, int32_t dtype,

@@ -88,7 +88,8 @@ def distill(logits, teacher_ids, teacher_logits, tau=1.0, teacher_lse=None, row_
         at = np.asarray(teacher_ids[i, there], dtype=np.int64)
         if lq is None or (teacher_lse is None and not there):
             bad_teacher = np.isnan(t).any() or np.isposinf(t).any() or \
-                (teacher_lse is None and bool(there) and np.isneginf(t).all())
+                (teacher_lse is None and bool(there) and np.isneginf(t).all()) or \
+                (teacher_lse is not None and not np.isfinite(teacher_lse[i]))
             if not bad_teacher:
                 continue
             lq = np.full(m, np.nan)
@@ -97,9 +98,9 @@ def distill(logits, teacher_ids, teacher_logits, tau=1.0, teacher_lse=None, row_
             lp = np.full(t.shape, np.nan) if lp is None else lp
         else:
             lp = t / tau - float(teacher_lse[i])
-            if np.isposinf(t).any():
+            if np.isposinf(t).any() or not np.isfinite(teacher_lse[i]):
                 lp = np.full(t.shape, np.nan)
-        if np.isnan(lp).any() or np.isnan(lq).any():
+        if np.isnan(lp).any() or np.isnan(lq).any() or (teacher_lse is not None and not np.isfinite(teacher_lse[i])):
             loss[i] = np.nan
             grad[i, :m] = np.nan
             continue

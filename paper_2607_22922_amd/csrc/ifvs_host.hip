@@ -2674,7 +2674,7 @@ ifvs_status ifvs_score_candidates(ifvs_index* idx, int32_t nq, const void* lut, 
   if (ifvs_status st = check_index(idx); st != IFVS_OK) return st;
   if (ifvs_status st = check_nq(idx, nq); st != IFVS_OK) return st;
   if (lut_dtype != IFVS_LUT_F32 && lut_dtype != IFVS_LUT_F16) return fail(IFVS_E_INVALID, "unknown lut_dtype");
-  if (n_cand < 1 || n_cand > IFVS_MAX_COLS) return fail(IFVS_E_INVALID, "n_cand must be in 1..2^21");
+  if (n_cand < 1 || n_cand > IFVS_MAX_COLS) return fail(IFVS_E_INVALID, "n_cand must be in 1..2^20");
   if (nq == 0) return IFVS_OK;
   if (!lut || !cand || !logits_out) return fail(IFVS_E_INVALID, "lut, cand or logits_out is NULL");
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -2708,7 +2708,7 @@ bool known_elem(int32_t dtype) {
 bool aligned_to(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 
 bool embed_sizes_ok(int64_t rows, int32_t dim, int64_t n, int32_t bag) {
-  return rows >= 1 && rows <= (int64_t(1) << 31) - 2 && dim >= 1 && dim <= (1 << 20) && bag >= 1 &&
+  return rows >= 1 && rows <= (int64_t(1) << 31) - 2 && dim >= 1 && dim <= 65536 && bag >= 1 &&
          bag <= IFVS_MAX_BAG && n >= 0 && n <= (int64_t(1) << 30) / bag;
 }
 
@@ -2728,7 +2728,7 @@ ifvs_status check_workspace(const void* workspace, int64_t have, int64_t need) {
 ifvs_status check_embed(int64_t rows, int32_t dim, int64_t n, int32_t bag, const int32_t* ids, float scale,
                         int32_t dtype) {
   if (!embed_sizes_ok(rows, dim, n, bag))
-    return fail(IFVS_E_INVALID, "rows, dim, bag or n * bag out of range (rows 1..2^31-2, dim 1..2^20, bag 1..16, "
+    return fail(IFVS_E_INVALID, "rows, dim, bag or n * bag out of range (rows 1..2^31-2, dim 1..65536, bag 1..16, "
                                 "n * bag 0..2^30)");
   if (!known_elem(dtype)) return fail(IFVS_E_INVALID, "unknown element type");
   if (!std::isfinite(scale)) return fail(IFVS_E_INVALID, "scale must be finite");
@@ -2739,7 +2739,7 @@ ifvs_status check_embed(int64_t rows, int32_t dim, int64_t n, int32_t bag, const
 // The checks that ifvs_log_probs and ifvs_distill_loss share.
 ifvs_status check_rows(int64_t n, int64_t cols, const void* logits, int64_t ld, int32_t dtype, const int32_t* n_valid,
                        float tau) {
-  if (!row_sizes_ok(n, cols)) return fail(IFVS_E_INVALID, "n or cols out of range (n 0..2^31-1, cols 1..2^21)");
+  if (!row_sizes_ok(n, cols)) return fail(IFVS_E_INVALID, "n or cols out of range (n 0..2^31-1, cols 1..2^20)");
   if (!known_elem(dtype)) return fail(IFVS_E_INVALID, "unknown element type");
   if (ld < cols) return fail(IFVS_E_INVALID, "the row stride of the logits is below cols");
   if (!(tau > 0.0f) || !std::isfinite(tau) || !std::isfinite(1.4426950408889634f / tau))

@@ -21,6 +21,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "ifvs.h"
 #include "rows_device.h"
 
 namespace ifvs {
@@ -30,7 +31,8 @@ namespace {
 constexpr double kLn2 = 0.69314718055994530942;
 constexpr float kExpFloor = -200.0f;            // 2^-200 is 0 in fp32
 constexpr float kHuge = 1e37f;
-constexpr int kMaxChunks = 64;                  // one per lane of the joining wavefront
+constexpr int kMaxChunks = 64;                  // one per lane of the joining wavefront; 2^20 fp32 columns are 64
+static_assert(IFVS_MAX_COLS / 4 <= kMaxChunks * 4096, "chunks of 4096 vectors");
 constexpr int64_t kMaxGrid = 1 << 22;           // workgroups of one launch
 constexpr int kListCap = 1024;                  // candidate columns a workgroup collects for its best
 constexpr int kGroups = 64;                     // thread groups whose maxima give the collecting threshold
@@ -457,21 +459,39 @@ struct DistillEnd {
   float loss;
 };
 
-// Dynamic LDS of the distillation: per slot the column relative to the chunk
-// (-1 elsewhere), the probabilities and the logit; then a bit per column.
+// Dynamic LDS of the distillation: per slot the probability, the logit and the
+// column relative to the chunk (-1 elsewhere); a hash table of the columns;
+// then a bit per column.
 struct TeacherLds {
   double* p;
   float* x;
   int* column;
+  int* hash;
+  int hash_bits;
   unsigned char* bits;
 };
+
+// At least twice as many entries as slots, so a probe always ends.
+__host__ __device__ constexpr int teacher_hash_bits(int n_teacher) {
+  int b = 6;
+  while ((1 << b) < 2 * n_teacher) ++b;
+  return b;
+}
+__host__ __device__ constexpr size_t teacher_slot_bytes(int n_teacher) {
+  return (static_cast<size_t>(n_teacher) * 16 + 15) & ~size_t{15};
+}
+__host__ __device__ constexpr size_t teacher_lds_bytes(int n_teacher) {
+  return teacher_slot_bytes(n_teacher) + (size_t{4} << teacher_hash_bits(n_teacher));
+}
 
 __device__ __forceinline__ TeacherLds teacher_lds(unsigned char* smem, int n_teacher) {
   TeacherLds t;
   t.p = reinterpret_cast<double*>(smem);
   t.x = reinterpret_cast<float*>(t.p + n_teacher);
   t.column = reinterpret_cast<int*>(t.x + n_teacher);
-  t.bits = smem + ((static_cast<size_t>(n_teacher) * 16 + 8 + 15) & ~size_t{15});
+  t.hash = reinterpret_cast<int*>(smem + teacher_slot_bytes(n_teacher));
+  t.hash_bits = teacher_hash_bits(n_teacher);
+  t.bits = smem + teacher_lds_bytes(n_teacher);
   return t;
 }
 
@@ -480,6 +500,7 @@ struct Teacher {
   double lse;          // natural logarithm of its sum
   double rest;         // P
   bool bad, present;
+  bool repeats;        // two slots name one column of the chunk
 };
 
 // One wavefront reads the slots; columns in [first, first + mine) are named.
@@ -501,11 +522,28 @@ __device__ __forceinline__ Teacher read_teacher(const DistillArgs& a, int64_t ro
     }
     t.column[k] = id >= first && id < first + mine ? id - first : -1;
   }
+  // Columns that several slots name are rare and cost comparing every pair
+  // (256 rows of 4096 columns, 128 slots: 28 us); a hash table says whether
+  // there are any.
   Teacher out;
+  for (int h = lane; h < (1 << t.hash_bits); h += 64) t.hash[h] = -1;
+  group_sync<64>();
+  bool repeats = false;
+  for (int k = lane; k < a.n_teacher; k += 64) {
+    const int column = t.column[k];
+    if (column < 0) continue;
+    for (uint32_t h = (static_cast<uint32_t>(column) * 2654435761u) >> (32 - t.hash_bits);; ++h) {
+      const int was = atomicCAS(&t.hash[h & ((1u << t.hash_bits) - 1)], -1, column);
+      repeats = repeats || was == column;
+      if (was == -1 || was == column) break;
+    }
+  }
+  out.repeats = __any(repeats);
   out.present = __any(present);
   mx = wave_max(mx);
   if (a.teacher_lse) {
     out.lse = a.teacher_lse[row];
+    if (!isfinite(out.lse)) bad = true;
   } else {
     if (out.present && mx == -INFINITY) bad = true;
     double sum = 0.0;
@@ -550,7 +588,8 @@ __device__ __forceinline__ DistillStat named_stat(const DistillArgs& a, int64_t 
     if (column < 0) continue;
     const double z = t.x[k] * a.c - mx, p = t.p[k];
     bool again = false;
-    for (int o = 0; o < k; ++o) again |= t.column[o] == column;
+    if (teacher.repeats)
+      for (int o = 0; o < k; ++o) again |= t.column[o] == column;
     if (!again) sum += pow2(z);
     if (p > 0.0) {
       loss += p * (logits[k] * inv_tau - teacher.lse - z * kLn2);
@@ -711,8 +750,11 @@ __device__ __forceinline__ void finish_named(const DistillArgs& a, int64_t row, 
   for (int k = tid; k < a.n_teacher; k += kThreads) {
     const int column = t.column[k];
     if (column < 0) continue;
-    double p = 0.0;
-    for (int o = 0; o < a.n_teacher; ++o) p += t.column[o] == column ? t.p[o] : 0.0;
+    double p = t.p[k];
+    if (teacher.repeats) {
+      p = 0.0;
+      for (int o = 0; o < a.n_teacher; ++o) p += t.column[o] == column ? t.p[o] : 0.0;
+    }
     const double q = pow2(t.x[k] * a.c - r.hi - log2_all);
     grad[column] = elem_round<T>(static_cast<float>(static_cast<double>(weight) * a.tau * (q - p)));
   }
@@ -1067,8 +1109,8 @@ template <typename T>
 hipError_t distill_typed(const DistillArgs& a, hipStream_t s) {
   const RowPlan p = distill_plan(a.n, a.cols, Elem<T>::kPerVec);
   DistillStat* stats = static_cast<DistillStat*>(a.workspace);
-  const size_t slots = static_cast<size_t>(a.n_teacher) * 16 + 8;
-  const size_t lds = ((slots + 15) & ~size_t{15}) + static_cast<size_t>(p.threads) * p.vecs + 32;
+  const size_t slots = teacher_lds_bytes(a.n_teacher);
+  const size_t lds = slots + static_cast<size_t>(p.threads) * p.vecs + 32;      // RowTile::kBitBytes, in words of 16
   const int64_t items = a.n * p.chunks;
   const hipError_t e = in_slices(items, [&](int64_t at, unsigned grid) {
     if (p.chunks > 1) {

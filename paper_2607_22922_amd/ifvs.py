@@ -32,7 +32,7 @@ OPT_COUNT_READS = 12
 OPT_COARSE = 13
 OPT_SCREEN = 14
 ELEM = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}     # IFVS_ELEM_*
-MAX_BAG, MAX_TOP, MAX_COLS = 16, 32, 1 << 21
+MAX_BAG, MAX_TOP, MAX_COLS = 16, 32, 1 << 20
 STAGES = ("condition", "lut", "filter", "scan", "merge", "encode", "coarse")
 
 EXPORTED = ("ifvs_load_index", "ifvs_free_index", "ifvs_select_codebook", "ifvs_build_lut",

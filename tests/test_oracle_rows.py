@@ -121,10 +121,10 @@ LOGP = dict(n=4, cols=50, logits=P, ld=50, dtype=0, n_valid=None, tau=1.0, given
 DISTILL = dict(n=4, cols=50, logits=P, ld=50, dtype=2, n_valid=None, n_teacher=3, ids=P, t=P, lse=None, tau=1.0,
                weight=None, loss=P, grad=P, grad_ld=50, ws=P, ws_bytes=W, stream=None)
 ODD = ctypes.c_void_p(0x1001)
-COMMON_ROWS = [("n", -1), ("n", 1 << 31), ("cols", 0), ("cols", (1 << 21) + 1), ("logits", None), ("logits", ODD),
+COMMON_ROWS = [("n", -1), ("n", 1 << 31), ("cols", 0), ("cols", (1 << 20) + 1), ("logits", None), ("logits", ODD),
                ("ld", 49), ("dtype", 3), ("dtype", -1), ("n_valid", ODD), ("tau", 0.0), ("tau", -1.0),
                ("tau", math.nan), ("tau", math.inf), ("tau", 1e-44)]
-EMBED = [("rows", 0), ("rows", (1 << 31) - 1), ("dim", 0), ("dim", (1 << 20) + 1), ("bag", 0), ("bag", 17),
+EMBED = [("rows", 0), ("rows", (1 << 31) - 1), ("dim", 0), ("dim", 65537), ("bag", 0), ("bag", 17),
          ("n", -1), ("n", (1 << 29) + 1), ("ids", None), ("ids", ODD), ("scale", math.nan), ("scale", math.inf),
          ("dtype", 3), ("out_ld", 7)]
 REFUSALS = (
@@ -153,9 +153,9 @@ def test_small_and_misaligned_workspaces_are_refused(B):
     lib = B.lib()
     for fn, good, need in (
             ("ifvs_embed_gradient", dict(GRAD, n=100000, rows=5000), lib.ifvs_embed_workspace(5000, 8, 100000, 2)),
-            ("ifvs_log_probs", dict(LOGP, n=2, cols=1 << 21, ld=1 << 21), lib.ifvs_log_probs_workspace(2, 1 << 21, 5)),
-            ("ifvs_distill_loss", dict(DISTILL, n=2, cols=1 << 21, ld=1 << 21, grad_ld=1 << 21),
-             lib.ifvs_distill_workspace(2, 1 << 21))):
+            ("ifvs_log_probs", dict(LOGP, n=2, cols=1 << 20, ld=1 << 20), lib.ifvs_log_probs_workspace(2, 1 << 20, 5)),
+            ("ifvs_distill_loss", dict(DISTILL, n=2, cols=1 << 20, ld=1 << 20, grad_ld=1 << 20),
+             lib.ifvs_distill_workspace(2, 1 << 20))):
         assert need >= 0
         if need == 0:
             continue
@@ -167,7 +167,7 @@ def test_workspace_sizes_out_of_range(B):
     lib = B.lib()
     assert lib.ifvs_embed_workspace(0, 8, 4, 1) == -1 and lib.ifvs_embed_workspace(8, 8, 4, 17) == -1
     assert lib.ifvs_log_probs_workspace(4, 0, 1) == -1 and lib.ifvs_log_probs_workspace(4, 9, 33) == -1
-    assert lib.ifvs_distill_workspace(-1, 9) == -1 and lib.ifvs_distill_workspace(1, (1 << 21) + 1) == -1
+    assert lib.ifvs_distill_workspace(-1, 9) == -1 and lib.ifvs_distill_workspace(1, (1 << 20) + 1) == -1
 
 
 def test_empty_calls_do_nothing(B):

@@ -136,6 +136,24 @@ def test_embed_gradient(B, dtype, out_dtype, rows, dim, n, bag, pad, shift, kind
     assert torch.all(acc[:, dim:] == 5)
 
 
+@pytest.mark.parametrize("dtype,out_dtype", [(torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16),
+                                             (torch.float16, torch.float32)])
+@pytest.mark.parametrize("rows,dim,pad", [(300, 33, 3), (5000, 520, 8), (41, 1, 1)])
+def test_embed_gradient_into_strided_rows(B, dtype, out_dtype, rows, dim, pad):
+    """Rows further apart than their length: cleared and written, what lies
+    between them is left."""
+    gen = _gen(rows)
+    grad = _row_view(60, dim, dtype, gen)
+    ids = torch.randint(-1, rows, (60, 2), generator=gen, device="cuda", dtype=torch.int32)
+    buf = torch.full((rows, dim + pad), 9.0, device="cuda", dtype=out_dtype)
+    out = buf[:, 1:1 + dim]
+    assert B.embed_gradient(grad, ids, rows, 1.5, out=out) is out
+    want = B.embed_gradient(grad, ids, rows, 1.5, dtype=out_dtype)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    assert torch.all(buf[:, :1] == 9) and torch.all(buf[:, 1 + dim:] == 9)
+
+
 def test_embed_gradient_of_no_slots_clears(B):
     out = torch.full((50, 7), 3.0, device="cuda")
     B.embed_gradient(torch.empty(0, 7, device="cuda"), torch.empty(0, 2, device="cuda", dtype=torch.int32), 50, out=out)
@@ -419,6 +437,71 @@ def test_distill_of_ragged_and_masked_rows(B, dtype, rest, cols):
     x[12] = x[12] * 0.25 + (1000 if dtype != torch.bfloat16 else 4096)
     t[13, 5] = -INF
     _check_distill(B, x, ids, t, 1.0, lse if rest else None, weight, n_valid)
+
+
+@pytest.mark.parametrize("rest", [False, True])
+def test_distill_of_repeated_and_undefined_teachers(B, rest):
+    """Slots that name one column many times, among more slots than a
+    wavefront's lanes; sums of the teacher that are not finite."""
+    gen = _gen(5)
+    x = _row_view(6, 900, torch.float32, gen)
+    ids, t, lse = _teacher(x, 200, 1.0, gen)
+    ids[0] = ids[0, 0]
+    ids[1, 100:] = ids[1, :100]
+    ids[2, 199] = ids[2, 0]
+    lse = lse + 1.0                            # repeats must not take more than everything
+    lse[4], lse[5] = float("nan"), INF
+    _check_distill(B, x, ids, t - (5.0 if rest else 0.0), 1.0, lse if rest else None)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_the_longest_rows(B, dtype):
+    """2^20 columns: the most chunks that a join takes."""
+    say(f"[longest] {dtype}")
+    cols = B.MAX_COLS
+    x = torch.randn(cols, generator=_gen(1), device="cuda").to(dtype).view(1, cols)
+    x[0, cols - 1] = 9.0
+    ids, t, lse = _teacher(x, 5, 1.0, _gen(2))
+    given, ent, top, logp = B.log_probs(x, ids, 4)
+    loss, grad = B.distill_loss(x, ids, t, 1.0, lse)
+    torch.cuda.synchronize()
+    lp = torch.log_softmax(x.double(), 1)
+    assert int(top[0, 0]) == cols - 1
+    # as _row_stats: u (3 E|z| + 132) with E|z| < 10, and the value's rounding
+    tol = U * (3 * 10 + 132 + 3 * 20)
+    assert torch.all((given.double() - torch.gather(lp, 1, ids.long())).abs() <= tol)
+    assert torch.all((logp.double() - torch.gather(lp, 1, top.long())).abs() <= tol)
+    assert abs(float(ent) + float((lp.exp() * lp).sum())) <= 20 * tol
+    w_loss, w_grad = R.distill(_np(x), _np(ids), _np(t), 1.0, _np(lse))
+    assert abs(float(loss) - w_loss[0]) <= 4 * tol
+    assert np.all(np.abs(_np(grad) - w_grad) <= (2 * tol + HALF[dtype] * 1.001) * np.abs(w_grad) + TINY[dtype] + U * 1e-6)
+
+
+def test_more_rows_than_one_grid_counts(B):
+    n = (1 << 22) + 37
+    x = torch.randn(n, 3, generator=_gen(4), device="cuda")
+    ids = torch.randint(0, 3, (n, 1), generator=_gen(5), device="cuda", dtype=torch.int32)
+    t = torch.zeros(n, 1, device="cuda")
+    given, ent, top, logp = B.log_probs(x, ids, 1)
+    loss, grad = B.distill_loss(x, ids, t)
+    torch.cuda.synchronize()
+    lp = torch.log_softmax(x.double(), 1)
+    at = torch.gather(lp, 1, ids.long())
+    tol = U * (3 * 12 + 8)                     # three terms a row, |z| below 12
+    assert torch.all((given.double() - at).abs() <= tol)
+    assert torch.equal(top[:, 0].long(), x.argmax(1))
+    assert torch.all((loss.double() + at[:, 0]).abs() <= tol)
+    hot = torch.zeros_like(lp).scatter_(1, ids.long(), 1.0)
+    assert torch.all((grad.double() - (lp.exp() - hot)).abs() <= tol)
+
+
+def test_empty_batches(B):
+    x = torch.empty(0, 7, device="cuda")
+    ids = torch.empty(0, 2, device="cuda", dtype=torch.int32)
+    assert B.embed_lookup(torch.ones(3, 7, device="cuda"), ids).shape == (0, 7)
+    assert [tuple(o.shape) for o in B.log_probs(x, ids, 4)] == [(0, 2), (0,), (0, 4), (0, 4)]
+    loss, grad = B.distill_loss(x, ids, torch.empty(0, 2, device="cuda"))
+    assert loss.shape == (0,) and grad.shape == (0, 7)
 
 
 def test_distill_far_from_the_teachers_columns(B):
