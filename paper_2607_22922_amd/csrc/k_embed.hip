@@ -55,6 +55,15 @@ struct LaneCols {
   // Elements of another type O at the same columns.
   template <typename O>
   __device__ __forceinline__ void load_old(const O* row, float* f) const {
+    constexpr int kO = Elem<O>::kPerVec;
+    if (own == kE) {
+#pragma unroll
+      for (int j = 0; j < kE; j += kO) {
+        const Word4 w = *reinterpret_cast<const Word4At2*>(row + start + j);
+        Elem<O>::unpack(w, f + j);
+      }
+      return;
+    }
     const int skip = narrow ? 0 : kE - own;
 #pragma unroll
     for (int j = 0; j < kE; ++j) f[j] = j >= skip && (!narrow || j < own) ? elem_load(row + start + j) : 0.0f;

@@ -186,9 +186,8 @@ struct BestLds {
 // full of ties) and ranked by counting.  Few threads hold such an element: they
 // lay their vectors out in LDS and their wavefront looks at them an element a
 // lane (2048 rows of 50001 fp16 logits, 10 alternatives: 48 us, each thread
-// looking at its own 54), except that where many lanes of a single wavefront
-// hold one each looks at its own (4096 rows of 1000, 32 alternatives: 11 us
-// against 18).  More than the list holds: one round over the
+// looking at its own 54), except that in short tiles many holders look at their
+// own each (4096 rows of 1000, 32 alternatives: 11 us against 18).  More than the list holds: one round over the
 // tile's len elements at x per rank.
 template <typename T, int kThreads, int kVecs, typename Emit>
 __device__ __forceinline__ void best_columns(RowTile<T, kThreads, kVecs>& tile, float thread_max,
@@ -214,7 +213,7 @@ __device__ __forceinline__ void best_columns(RowTile<T, kThreads, kVecs>& tile, 
   keep(tile.edge, tile.edge_column());
   uint64_t holders = __ballot(thread_max >= threshold && thread_max > -INFINITY);
   tile.forget_unpacked();
-  if (kThreads > 64 || __popcll(holders) <= kStaged) {
+  if (kVecs > 8 || __popcll(holders) <= kStaged) {
     while (holders != 0) {
       const int mine = __popcll(holders & ((1ull << lane) - 1));
       if (((holders >> lane) & 1u) && mine < kStaged) {

@@ -580,8 +580,10 @@ def _rows_arg(t, name):
     rows that do not overlap; other layouts are copied."""
     if t.dim() != 2 or not t.is_cuda or t.dtype not in ELEM:
         raise IfvsError(E_INVALID, f"{name} must be a 2-D CUDA tensor of float32, float16 or bfloat16")
-    if t.shape[0] > 1 and t.stride(0) < t.shape[1] or t.shape[1] > 1 and t.stride(1) != 1:
-        t = t.contiguous()
+    if not t.is_contiguous():
+        n, cols = t.shape
+        if n > 1 and t.stride(0) < cols or cols > 1 and t.stride(1) != 1:
+            t = t.contiguous()
     return t
 
 
