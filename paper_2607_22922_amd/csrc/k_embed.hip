@@ -598,6 +598,63 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(const Embed
   put_row<O>(a, LaneCols<T>(vec, a.dim), run, sum);
 }
 
+// Few slots: one workgroup per sorted slot and 64 vectors of columns sums the
+// run that starts at the slot (others leave at once), its four wavefronts a
+// quarter each, so one launch does without pieces and joins (512 slots of 384
+// columns: 14 us against 17; a run of all 1024 slots 44 against 21).
+constexpr int64_t kRunSlots = 1024;
+template <typename T, typename O>
+__global__ __launch_bounds__(64 * kJoinWaves) void embed_run_kernel(const EmbedArgs a, const SumArgs s,
+                                                                    int col_blocks) {
+  constexpr int kE = Elem<T>::kPerVec;
+  __shared__ float s_sum[kJoinWaves - 1][kE][64];
+  const int slots = static_cast<int>(s.slots);
+  const int e = static_cast<int>(blockIdx.x) / col_blocks;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint32_t run = s.key[e];
+  if (run >= static_cast<uint32_t>(a.rows) || (e > 0 && s.key[e - 1] == run)) return;
+  int count = 0;
+  for (int at = e;; at += 64 * kJoinWaves) {
+    const int n = __syncthreads_count(at + tid < slots && s.key[min(at + tid, slots - 1)] == run ? 1 : 0);
+    count += n;
+    if (n < 64 * kJoinWaves) break;
+  }
+  const int vec = static_cast<int>(blockIdx.x) % col_blocks * 64 + lane;
+  const bool live = vec * kE < a.dim;
+  const LaneCols<T> cols(live ? vec : 0, a.dim);
+  float sum[kE];
+#pragma unroll
+  for (int j = 0; j < kE; ++j) sum[j] = 0.0f;
+  const int hi = e + count * (wave + 1) / kJoinWaves;
+  for (int at = e + count * wave / kJoinWaves; at < hi; at += kAhead) {
+    uint32_t from[kAhead];
+    Word4 w[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) from[u] = s.from[min(at + u, hi - 1)];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      w[u] = cols.load_raw(static_cast<const T*>(a.grad) + static_cast<int64_t>(from[u]) * a.grad_ld);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (at + u < hi) {
+        float f[kE];
+        Elem<T>::unpack(w[u], f);
+#pragma unroll
+        for (int j = 0; j < kE; ++j) sum[j] += f[j];
+      }
+  }
+  if (wave > 0)
+#pragma unroll
+    for (int j = 0; j < kE; ++j) s_sum[wave - 1][j][lane] = sum[j];
+  __syncthreads();
+  if (wave > 0 || !live) return;
+#pragma unroll
+  for (int q = 0; q < kJoinWaves - 1; ++q)
+#pragma unroll
+    for (int j = 0; j < kE; ++j) sum[j] += s_sum[q][j][lane];
+  put_row<O>(a, cols, run, sum);
+}
+
 // ---------------------------------------------------------------- the plan
 struct EmbedPlan {
   int bits, passes, groups;          // passes 0: sort_owned_kernel, groups owners
@@ -628,7 +685,7 @@ EmbedPlan embed_plan(int64_t rows, int dim, int64_t slots) {
   p.piece = static_cast<int>(round_up(
       std::max({std::min((slots + kPieces - 1) / kPieces, kLongPiece), (slots + kMaxPieces - 1) / kMaxPieces, int64_t{1}}),
       kAhead));
-  p.pieces = (slots + p.piece - 1) / p.piece;
+  p.pieces = slots <= kRunSlots ? 0 : (slots + p.piece - 1) / p.piece;
   p.pitch = static_cast<int>(round_up(dim, 8));
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
@@ -744,6 +801,11 @@ hipError_t gradient_typed(const EmbedArgs& a, hipStream_t s) {
   sum.pitch = p.pitch;
   sum.lanes = lanes_per_row(vecs);
   sum.col_blocks = (vecs + kEmbThreads - 1) / kEmbThreads;
+  if (slots <= kRunSlots) {
+    const int col_blocks = (vecs + 63) / 64;
+    embed_run_kernel<T, O><<<static_cast<unsigned>(slots * col_blocks), 64 * kJoinWaves, 0, s>>>(a, sum, col_blocks);
+    return hipGetLastError();
+  }
   const int groups = kEmbThreads / sum.lanes;
   embed_sum_kernel<T, O><<<static_cast<unsigned>((p.pieces + groups - 1) / groups * sum.col_blocks), kEmbThreads, 0,
                            s>>>(a, sum);

@@ -101,7 +101,8 @@ def test_embed_lookup(B, dtype, rows, dim, n, bag, pad, shift):
     (3000, 40, 5000, 1, 0, 0, "one"), (200, 33, 4097, 2, 1, 1, "skew"), (70000, 8, 300, 1, 0, 0, "any"),
     (20, 16, 50, 3, 0, 0, "absent"), (9, 700, 1, 16, 0, 0, "any"), (150000, 24, 9001, 1, 0, 0, "skew"),
     (600000, 5, 300, 2, 0, 0, "any"), (600000, 9, 9001, 1, 0, 0, "skew"), (1500, 12, 70001, 2, 1, 0, "any"),
-    (77, 20, 150000, 1, 0, 0, "skew"), (5000, 36, 33000, 1, 0, 0, "skew"), (3000, 6, 140001, 1, 0, 0, "one")])
+    (77, 20, 150000, 1, 0, 0, "skew"), (5000, 36, 33000, 1, 0, 0, "skew"), (3000, 6, 140001, 1, 0, 0, "one"),
+    (90, 1100, 1024, 1, 0, 0, "skew"), (90, 70, 1025, 1, 1, 0, "skew"), (50, 600, 512, 2, 0, 1, "one")])
 def test_embed_gradient(B, dtype, out_dtype, rows, dim, n, bag, pad, shift, kind):
     say(f"[gradient] {dtype}->{out_dtype} rows={rows} dim={dim} n={n} bag={bag} {kind}")
     gen = _gen(rows + dim)
