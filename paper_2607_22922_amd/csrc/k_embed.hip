@@ -138,8 +138,14 @@ constexpr int kSortTile = kSortThreads * kSortRounds;
 constexpr int kSortMaxBits = 10;
 constexpr int kSortMaxGroups = 256;
 // One launch (sort_owned_kernel) up to this many slots and owners: each owner
-// reads all ids twice, so its time grows with slots x owners.
-constexpr int64_t kOwnedSlots = 1 << 17;
+// reads all ids, so its time grows with slots x owners, and the owner of a
+// frequent row sorts alone.  Gradients of 64 columns, uniform and skewed ids, us,
+// one launch against four: 8192 slots 21 and 31, 34 and 43; 16384 26 and 44, 37
+// and 48; 32768 40 and 75, 42 and 52; 131072 104 and 255, 51 and 88.  Twice as
+// many where a large table is cleared beside it anyway (21003 slots and 173 MB
+// 52 and 63, 32768 and 537 MB 142 and 148).
+constexpr int64_t kOwnedSlots = 1 << 14;
+constexpr int64_t kLongClear = 1 << 27;               // bytes
 constexpr int kOwnersFull = 256;
 constexpr int64_t kMostOwners = 1 << 9;
 
@@ -279,13 +285,22 @@ struct ClearArgs {
   char* out;
   int64_t rows, row_bytes, stride, last_bytes;   // rows of row_bytes, the last one of last_bytes
   int threads;                                    // of a row: a workgroup or a wavefront
-  int64_t blocks;
+  int64_t row0, row1, blocks;                     // a launch's share of them and its workgroups
 };
+
+// Share `k` of `of` equal ones.
+ClearArgs clear_share(ClearArgs c, int64_t k, int64_t of) {
+  const int64_t per = kSortThreads / c.threads;
+  c.row0 = c.rows * k / of;
+  c.row1 = c.rows * (k + 1) / of;
+  c.blocks = std::min<int64_t>((c.row1 - c.row0 + per - 1) / per, 1 << 20);
+  return c;
+}
 
 __device__ __forceinline__ void clear_rows(const ClearArgs& c, int64_t block) {
   const Word4 zero{0, 0, 0, 0};
   const int per = kSortThreads / c.threads, lane = threadIdx.x & (c.threads - 1);
-  for (int64_t r = block * per + threadIdx.x / c.threads; r < c.rows; r += c.blocks * per) {
+  for (int64_t r = c.row0 + block * per + threadIdx.x / c.threads; r < c.row1; r += c.blocks * per) {
     char* out = c.out + r * c.stride;
     const int64_t bytes = r == c.rows - 1 ? c.last_bytes : c.row_bytes;
     const int64_t vecs = bytes >> 4;
@@ -398,8 +413,12 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs
   if (threadIdx.x < (1u << a.bits)) a.hist[(blockIdx.x << a.bits) + threadIdx.x] = s.base[threadIdx.x];
 }
 
-__global__ __launch_bounds__(kSortThreads) void sort_move_kernel(const SortArgs a, int first) {
+__global__ __launch_bounds__(kSortThreads) void sort_move_kernel(const SortArgs a, int first, const ClearArgs c) {
   __shared__ SortLds s;
+  if (static_cast<int>(blockIdx.x) >= a.groups) {
+    clear_rows(c, blockIdx.x - a.groups);
+    return;
+  }
   const int tid = threadIdx.x;
   uint32_t total = 0, before = 0;
   constexpr int kAtOnce = 8;
@@ -666,13 +685,14 @@ struct EmbedPlan {
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
-EmbedPlan embed_plan(int64_t rows, int dim, int64_t slots) {
+// clear_bytes: of the table's gradient (0: needs the most workspace).
+EmbedPlan embed_plan(int64_t rows, int dim, int64_t slots, int64_t clear_bytes) {
   EmbedPlan p{};
   int bits = 1;
   while ((rows >> bits) != 0) ++bits;                 // `rows` itself is a key
   int own = 6;
   while (own < kSortMaxBits && (rows >> own) >= kOwnersFull) ++own;
-  if (slots <= kOwnedSlots && (rows >> own) < kMostOwners) {
+  if (slots <= (clear_bytes >= kLongClear ? 2 : 1) * kOwnedSlots && (rows >> own) < kMostOwners) {
     p.bits = own;
     p.groups = static_cast<int>((rows >> own) + 1);
   } else {
@@ -722,7 +742,7 @@ hipError_t lookup_typed(const EmbedArgs& a, hipStream_t s) {
   return hipSuccess;
 }
 
-// Sorts the slots; its first launch clears the table beside it (c.blocks 0: not).
+// Sorts the slots; its launches clear the table beside it (c.rows 0: nothing).
 hipError_t sort_slots(const EmbedArgs& a, const EmbedPlan& p, int64_t slots, char* ws, const ClearArgs& c,
                       hipStream_t s, SumArgs& sum) {
   SortArgs o{};
@@ -742,18 +762,20 @@ hipError_t sort_slots(const EmbedArgs& a, const EmbedPlan& p, int64_t slots, cha
   if (p.passes == 0) {
     o.in = buf[1];
     o.out = buf[0];
-    sort_owned_kernel<<<static_cast<unsigned>(p.groups + c.blocks), kSortThreads, 0, s>>>(o, c);
+    const ClearArgs all = clear_share(c, 0, 1);
+    sort_owned_kernel<<<static_cast<unsigned>(p.groups + all.blocks), kSortThreads, 0, s>>>(o, all);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   } else {
+    const int launches = 2 * p.passes;
     for (int pass = 0; pass < p.passes; ++pass) {
       to = pass & 1;
       o.shift = pass * p.bits;
       o.in = buf[to ^ 1];
       o.out = buf[to];
-      const int64_t blocks = p.groups + (pass == 0 ? c.blocks : 0);
-      sort_count_kernel<<<static_cast<unsigned>(blocks), kSortThreads, 0, s>>>(o, pass == 0, c);
+      const ClearArgs one = clear_share(c, 2 * pass, launches), two = clear_share(c, 2 * pass + 1, launches);
+      sort_count_kernel<<<static_cast<unsigned>(p.groups + one.blocks), kSortThreads, 0, s>>>(o, pass == 0, one);
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-      sort_move_kernel<<<p.groups, kSortThreads, 0, s>>>(o, pass == 0);
+      sort_move_kernel<<<static_cast<unsigned>(p.groups + two.blocks), kSortThreads, 0, s>>>(o, pass == 0, two);
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
   }
@@ -765,7 +787,7 @@ hipError_t sort_slots(const EmbedArgs& a, const EmbedPlan& p, int64_t slots, cha
 template <typename T, typename O>
 hipError_t gradient_typed(const EmbedArgs& a, hipStream_t s) {
   const int64_t slots = a.n * a.bag;
-  const EmbedPlan p = embed_plan(a.rows, a.dim, slots);
+  const EmbedPlan p = embed_plan(a.rows, a.dim, slots, a.accumulate ? 0 : a.rows * a.dim * static_cast<int64_t>(sizeof(O)));
   char* ws = static_cast<char*>(a.workspace);
   ClearArgs c{};
   c.out = static_cast<char*>(a.out);
@@ -785,11 +807,11 @@ hipError_t gradient_typed(const EmbedArgs& a, hipStream_t s) {
     c.last_bytes = all - (c.rows - 1) * c.stride;
     c.threads = kSortThreads;
   }
-  const int64_t per_block = kSortThreads / c.threads;
-  c.blocks = a.accumulate ? 0 : std::min<int64_t>((c.rows + per_block - 1) / per_block, 1 << 20);
+  if (a.accumulate) c.rows = 0;
   SumArgs sum{};
   if (slots == 0) {
-    clear_kernel<<<static_cast<unsigned>(c.blocks), kSortThreads, 0, s>>>(c);
+    const ClearArgs all = clear_share(c, 0, 1);
+    clear_kernel<<<static_cast<unsigned>(all.blocks), kSortThreads, 0, s>>>(all);
     return hipGetLastError();
   }
   if (hipError_t e = sort_slots(a, p, slots, ws, c, s, sum); e != hipSuccess) return e;
@@ -817,7 +839,7 @@ hipError_t gradient_typed(const EmbedArgs& a, hipStream_t s) {
 
 }  // namespace
 
-int64_t embed_workspace_bytes(int64_t rows, int dim, int64_t slots) { return embed_plan(rows, dim, slots).bytes; }
+int64_t embed_workspace_bytes(int64_t rows, int dim, int64_t slots) { return embed_plan(rows, dim, slots, 0).bytes; }
 
 hipError_t launch_embed_lookup(const EmbedArgs& a, hipStream_t s) {
   if (a.n == 0) return hipSuccess;

@@ -102,12 +102,13 @@ def test_embed_lookup(B, dtype, rows, dim, n, bag, pad, shift):
     (20, 16, 50, 3, 0, 0, "absent"), (9, 700, 1, 16, 0, 0, "any"), (150000, 24, 9001, 1, 0, 0, "skew"),
     (600000, 5, 300, 2, 0, 0, "any"), (600000, 9, 9001, 1, 0, 0, "skew"), (1500, 12, 70001, 2, 1, 0, "any"),
     (77, 20, 150000, 1, 0, 0, "skew"), (5000, 36, 33000, 1, 0, 0, "skew"), (3000, 6, 140001, 1, 0, 0, "one"),
-    (90, 1100, 1024, 1, 0, 0, "skew"), (90, 70, 1025, 1, 1, 0, "skew"), (50, 600, 512, 2, 0, 1, "one")])
+    (90, 1100, 1024, 1, 0, 0, "skew"), (90, 70, 1025, 1, 1, 0, "skew"), (50, 600, 512, 2, 0, 1, "one"),
+    (130000, 600, 20000, 1, 0, 0, "skew")])
 def test_embed_gradient(B, dtype, out_dtype, rows, dim, n, bag, pad, shift, kind):
     say(f"[gradient] {dtype}->{out_dtype} rows={rows} dim={dim} n={n} bag={bag} {kind}")
     gen = _gen(rows + dim)
     grad = _row_view(n, dim, dtype, gen, pad, shift, 1.0)
-    # past 131072 slots or 512K rows the sort takes several launches
+    # past 16384 slots (32768 beside a large table) or 512K rows the sort takes several launches
     ids = torch.randint(-2, rows + 2, (n, bag), generator=gen, device="cuda", dtype=torch.int32)
     if kind == "one":
         ids[:] = rows - 1
