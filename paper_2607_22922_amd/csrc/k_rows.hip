@@ -152,15 +152,17 @@ __device__ __forceinline__ uint64_t wave_key_max(uint64_t v) {
   return key_max(key_max(key_lane(v, 0), key_lane(v, 16)), key_max(key_lane(v, 32), key_lane(v, 48)));
 }
 
-// A value that at least nth of a wavefront's 64 values reach: the nth largest,
-// rounded down to bf16.  A bisection over its 16 leading bits, a comparison and
-// a count of lanes each (64 comparisons with every lane's value cost three
-// times the vector instructions).
+// The nth largest (1-based) of a wavefront's 64 values, for 16-bit elements a
+// value just below it.  A bisection over the bits that an element has, a
+// comparison and a count of lanes each (64 comparisons with every lane's value
+// cost three times the vector instructions; fewer bits than the element's
+// would let rows far from 0 pass whole).
+template <int kLowBit>
 __device__ __forceinline__ float reached_by(float v, int nth) {
   const uint32_t key = ordered_bits(v);
   uint32_t cut = 0;
 #pragma unroll
-  for (int b = 31; b >= 16; --b) {
+  for (int b = 31; b >= kLowBit; --b) {
     const uint32_t t = cut | (1u << b);
     if (__popcll(__ballot(key >= t)) >= nth) cut = t;
   }
@@ -203,7 +205,7 @@ __device__ __forceinline__ void best_columns(RowTile<T, kThreads, kVecs>& tile, 
   if (tid % kPer == 0) s.group[tid / kPer] = g;
   if (tid == 0) s.count = 0;
   group_sync<kThreads>();
-  const float threshold = reached_by(s.group[lane], n_top);
+  const float threshold = reached_by<Elem<T>::kLowBit>(s.group[lane], n_top);
   auto keep = [&](float f, int column) {
     if (f >= threshold && f > -INFINITY) {
       const int at = atomicAdd(&s.count, 1);
@@ -260,7 +262,43 @@ __device__ __forceinline__ void best_columns(RowTile<T, kThreads, kVecs>& tile, 
       }
   }
   group_sync<kThreads>();
-  const int m = s.count;
+  int m = s.count;
+  if (m > kListCap) {
+    // A row full of equal logits: the same with keys, in which no two columns
+    // are equal, from memory (the tile would cost every row registers).
+    group_sync<kThreads>();
+    uint64_t key = 0;
+    if (thread_max > -INFINITY) {
+      int lowest = 0x7FFFFFFF;
+      tile.each_vector_from_memory(x, [&](float f, int column) {
+        if (f == thread_max) lowest = min(lowest, column);
+        return lowest == 0x7FFFFFFF;
+      });
+      key = column_key(thread_max, first_column + lowest);
+    }
+    s.list[tid] = key;
+    if (tid == 0) s.count = 0;
+    group_sync<kThreads>();
+    uint64_t group = 0;
+#pragma unroll
+    for (int r = 0; r < kPer; ++r) group = key_max(group, s.list[lane * kPer + r]);
+    int greater = 0;
+    for (int o = 0; o < 64; ++o) greater += key_lane(group, o) > group ? 1 : 0;
+    // fewer than n_top groups with a key: every element
+    const uint64_t at = __ballot(greater == n_top - 1 && group != 0);
+    const uint64_t cut = at != 0 ? key_lane(group, __builtin_ctzll(at)) : 1;
+    group_sync<kThreads>();
+    if (key >= cut)
+      tile.each_vector_from_memory(x, [&](float f, int column) {
+        if (f > -INFINITY && column_key(f, first_column + column) >= cut) {
+          const int to = atomicAdd(&s.count, 1);
+          if (to < kListCap) s.list[to] = column_key(f, first_column + column);
+        }
+        return true;
+      });
+    group_sync<kThreads>();
+    m = s.count;
+  }
   if (m <= kListCap) {
     for (int e = tid; e < m; e += kThreads) {
       const uint64_t key = s.list[e];

@@ -35,6 +35,7 @@ template <typename T>
 struct Elem;
 template <>
 struct Elem<float> {
+  static constexpr int kLowBit = 0;          // of an element's fp32 bits: below it all are 0
   static constexpr int kPerVec = 4;
   static constexpr uint32_t kNegInfWord = 0xFF800000u;
   static __device__ __forceinline__ void unpack(const Word4& w, float* f) {
@@ -50,6 +51,7 @@ struct Elem<float> {
 };
 template <>
 struct Elem<_Float16> {
+  static constexpr int kLowBit = 13;          // of an element's fp32 bits: below it all are 0
   static constexpr int kPerVec = 8;
   static constexpr uint32_t kNegInfWord = 0xFC00FC00u;
   static __device__ __forceinline__ void unpack(const Word4& w, float* f) {
@@ -68,6 +70,7 @@ struct Elem<_Float16> {
 };
 template <>
 struct Elem<__bf16> {
+  static constexpr int kLowBit = 16;          // of an element's fp32 bits: below it all are 0
   static constexpr int kPerVec = 8;
   static constexpr uint32_t kNegInfWord = 0xFF80FF80u;
   static __device__ __forceinline__ void unpack(const Word4& w, float* f) {
@@ -217,6 +220,24 @@ struct RowTile {
 #pragma unroll 1
         for (int j = 0; j < kE; ++j) f(elem_load(x + column(i, j)), column(i, j));
     if (static_cast<int>(threadIdx.x) < nedge) f(elem_load(x + edge_column()), edge_column());
+  }
+
+  // The same a vector a load, columns ascending but for the edge's, until f
+  // returns false.
+  template <typename F>
+  __device__ __forceinline__ void each_vector_from_memory(const T* x, F&& f) const {
+    const int tid = threadIdx.x;
+    if (tid < nedge && !f(elem_load(x + edge_column()), edge_column()) && tid < head) return;
+#pragma unroll 1
+    for (int i = 0; i < kVecs; ++i) {
+      if (tid >= nvec - i * kThreads) return;
+      float y[kE];
+      Elem<T>::unpack(load_words_again(x + column(i, 0)), y);
+      bool more = true;
+#pragma unroll
+      for (int j = 0; j < kE; ++j) more = f(y[j], column(i, j)) && more;
+      if (!more) return;
+    }
   }
 
   // Between two passes over the tile: the compiler would keep every unpacked

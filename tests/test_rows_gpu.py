@@ -295,12 +295,14 @@ def test_alternatives_of_tied_rows(B, dtype, cols):
     best columns all lie side by side."""
     say(f"[ties] {dtype} cols={cols}")
     gen = _gen(cols)
-    x = torch.zeros(6, cols, device="cuda")
+    x = torch.zeros(7, cols, device="cuda")
     x[1] = torch.randint(0, 3, (cols,), generator=gen, device="cuda").float()
     x[2, ::3] = -0.0
     x[3, cols // 2:cols // 2 + 40] = 4.0
     x[4] = -torch.arange(cols, device="cuda") / 64.0
     x[5] = torch.arange(cols, device="cuda") / 64.0
+    # thousands of equal best columns, all held by a few threads
+    x[6] = torch.where(torch.arange(cols, device="cuda") // 8 % 256 < 32, 1.0, -1.0 - torch.rand(cols, device="cuda"))
     _check_log_probs(B, x.to(dtype), 1.0, None, None, 32)
     _check_log_probs(B, x.to(dtype), 1.0, None, None, 1)
 
