@@ -453,6 +453,8 @@ class Index:
         """[nq][n_cand] logits of the candidates (ids, -1 absent) under the
         tables, for log_probs and distill_loss."""
         cand = cand.to(dtype=torch.int32).contiguous()
+        if lut.shape[0] != cand.shape[0]:
+            raise IfvsError(E_INVALID, "lut and cand have different row counts")
         logits = torch.empty(cand.shape, device=self.device)
         self.score_candidates_into(cand.shape[0], lut, lut_dtype, cand, logits)
         return logits
@@ -473,6 +475,8 @@ class Index:
         teacher_dist = _dev_f32(teacher_dist, self.device)
         if cand.shape[0] != q.shape[0] or teacher_dist.shape[0] != q.shape[0]:
             raise IfvsError(E_INVALID, "q, cand and teacher_dist have different row counts")
+        if w_z is not None and w_z.shape != q.shape:
+            raise IfvsError(E_INVALID, "w_z must have q's shape")
         loss = torch.empty(q.shape[0], device=self.device)
         dwz = torch.empty_like(q) if want_dwz else None
         self.distill_step_into(q, pack_predicates(preds), None if w_z is None else w_z.contiguous(), cand,
@@ -706,6 +710,8 @@ def log_probs(logits, given=None, n_top=0, tau=1.0, n_valid=None):
     n, cols = logits.shape
     n_top = int(n_top)
     with _OnDevice(dev):
+        if given is not None and given.dim() != 2:
+            raise IfvsError(E_INVALID, "given must be [n][n_given]")
         n_given = 0 if given is None else given.shape[1]
         given = _small_arg(given, "given", torch.int32, (n, n_given), dev)
         n_valid = _small_arg(n_valid, "n_valid", torch.int32, (n,), dev)
@@ -728,6 +734,8 @@ def distill_loss(logits, teacher_ids, teacher_logits, tau=1.0, teacher_lse=None,
     rows = _rows_arg(logits, "logits")
     dev = rows.device
     n, cols = rows.shape
+    if teacher_ids.dim() != 2:
+        raise IfvsError(E_INVALID, "teacher_ids must be [n][n_teacher]")
     with _OnDevice(dev):
         k = teacher_ids.shape[1]
         teacher_ids = _small_arg(teacher_ids, "teacher_ids", torch.int32, (n, k), dev)

@@ -136,6 +136,11 @@ def test_distill_step_refusals(B):
     with pytest.raises(B.IfvsError) as e:
         plain.score_candidates(plain.build_lut(q), cand[:, :0])
     assert e.value.status == B.E_INVALID
+    for call in (lambda: plain.score_candidates(plain.build_lut(q), cand[:5]),
+                 lambda: idx.distill_step(q, preds, w_z[:5], cand, t, 1.0, 0.1, 1.0)):
+        with pytest.raises(B.IfvsError) as e:
+            call()
+        assert e.value.status == B.E_INVALID
     torch.cuda.synchronize()
     bank1, W1 = idx.read_params()
     assert torch.equal(bank0, bank1) and torch.equal(W0, W1)

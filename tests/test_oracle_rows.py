@@ -176,3 +176,10 @@ def test_empty_calls_do_nothing(B):
     assert lib.ifvs_embed_gradient(*dict(GRAD, n=0, accumulate=1).values()) == B.OK
     assert lib.ifvs_log_probs(*dict(LOGP, n=0).values()) == B.OK
     assert lib.ifvs_distill_loss(*dict(DISTILL, n=0).values()) == B.OK
+
+
+def test_index_calls_need_a_handle(B):
+    lib = B.lib()
+    assert lib.ifvs_score_candidates(None, 1, P, 0, P, 4, P, None) == B.E_STATE
+    assert lib.ifvs_distill_step(None, 1, P, P, None, P, 4, 2, P, 1.0, 0.0, 0.1, P, None, None) == B.E_STATE
+    assert b"NULL" in lib.ifvs_last_error()

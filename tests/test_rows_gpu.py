@@ -239,7 +239,8 @@ def _check_log_probs(B, logits, tau=1.0, n_valid=None, given=None, n_top=0):
     (1, 1, 1, 1, 0, 0, 1.0), (3, 2, 2, 5, 0, 0, 0.5), (5, 7, 3, 3, 1, 1, 1.0), (9, 42, 10, 32, 0, 0, 1.0),
     (70, 64, 1, 1, 0, 0, 2.0), (4, 100, 0, 0, 3, 2, 1.0), (6, 1000, 100, 20, 0, 1, 0.7), (3, 1023, 1, 32, 1, 0, 1.0),
     (5, 4096, 7, 10, 0, 0, 1.0), (3, 4099, 1, 0, 0, 3, 1.0), (2, 8193, 1, 7, 0, 0, 1.0), (2, 50001, 1, 32, 0, 0, 1.0),
-    (1, 131072, 1, 20, 0, 0, 0.8), (300, 700, 1, 5, 0, 0, 1.0), (2, 40000, 1024, 1, 7, 5, 1.3)])
+    (1, 131072, 1, 20, 0, 0, 0.8), (300, 700, 1, 5, 0, 0, 1.0), (2, 40000, 1024, 1, 7, 5, 1.3),
+    (270, 40001, 2, 9, 1, 1, 1.0), (3, 28000, 1, 32, 0, 2, 1.0)])
 def test_log_probs(B, dtype, n, cols, n_given, n_top, pad, shift, tau):
     say(f"[logprobs] {dtype} n={n} cols={cols} given={n_given} top={n_top}")
     gen = _gen(n + cols)
@@ -399,7 +400,7 @@ def _teacher(x, k, tau, gen, n_valid=None):
     (1, 1, 1, 0, 0, 1.0), (3, 2, 1, 0, 0, 2.0), (5, 7, 7, 1, 1, 1.0), (9, 42, 10, 0, 0, 1.0), (70, 64, 5, 0, 0, 4.0),
     (6, 1000, 100, 0, 1, 0.7), (3, 1023, 30, 1, 0, 1.0), (5, 4096, 64, 0, 0, 2.0), (3, 4099, 8, 0, 3, 1.0),
     (2, 8193, 1024, 0, 0, 1.0), (2, 50001, 32, 0, 0, 2.0), (1, 131072, 64, 0, 0, 1.0), (300, 700, 12, 0, 0, 1.0),
-    (2, 40000, 20, 7, 5, 1.0)])
+    (2, 40000, 20, 7, 5, 1.0), (130, 40001, 17, 1, 1, 1.0), (515, 5001, 9, 0, 1, 2.0), (513, 20003, 9, 2, 0, 1.0)])
 def test_distill(B, dtype, rest, n, cols, k, pad, shift, tau):
     say(f"[distill] {dtype} n={n} cols={cols} k={k} rest={rest}")
     gen = _gen(n + cols)
@@ -411,14 +412,13 @@ def test_distill(B, dtype, rest, n, cols, k, pad, shift, tau):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rest", [False, True])
-@pytest.mark.parametrize("cols", [50, 3001, 40001])
-def test_distill_of_ragged_and_masked_rows(B, dtype, rest, cols):
+@pytest.mark.parametrize("cols,n", [(50, 14), (3001, 14), (40001, 14), (40001, 131), (9001, 514)])
+def test_distill_of_ragged_and_masked_rows(B, dtype, rest, cols, n):
     """Rows left out by weight, length or mask (with NaN where nothing is
     read), absent and repeated teacher slots, a listed column of probability 0
     (an infinite loss), undefined rows and teachers."""
     say(f"[distill masks] {dtype} cols={cols} rest={rest}")
     gen = _gen(cols)
-    n = 14
     x = _row_view(n, cols, dtype, gen)
     n_valid = torch.full((n,), cols, device="cuda", dtype=torch.int32)
     n_valid[1], n_valid[2], n_valid[3] = 0, 1, cols // 2
@@ -592,6 +592,7 @@ def test_wrapper_refusals(B):
     t = torch.zeros(4, 2, device="cuda")
     for call in (lambda: B.log_probs(x.cpu()), lambda: B.log_probs(x.double()), lambda: B.log_probs(x[0]),
                  lambda: B.log_probs(x, ids[:3]), lambda: B.log_probs(x, ids.cpu()), lambda: B.log_probs(x, n_top=33),
+                 lambda: B.log_probs(x, ids[:, 0]), lambda: B.distill_loss(x, ids[:, 0], t),
                  lambda: B.log_probs(x, ids.float()), lambda: B.log_probs(x, n_valid=ids[:, 0][:2]),
                  lambda: B.distill_loss(x, ids, t[:, :1]), lambda: B.distill_loss(x, ids, t, tau=0.0),
                  lambda: B.distill_loss(x, ids, t, grad_out=torch.empty(4, 9, device="cuda")),
