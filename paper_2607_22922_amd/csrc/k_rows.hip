@@ -189,8 +189,9 @@ struct BestLds {
 // lay their vectors out in LDS and their wavefront looks at them an element a
 // lane (2048 rows of 50001 fp16 logits, 10 alternatives: 48 us, each thread
 // looking at its own 54), except that in short tiles many holders look at their
-// own each (4096 rows of 1000, 32 alternatives: 11 us against 18).  More than the list holds: one round over the
-// tile's len elements at x per rank.
+// own each (4096 rows of 1000, 32 alternatives: 11 us against 18).  More than the
+// list holds: collected again by key from memory, and where that is too much too,
+// one round over the tile's len elements at x per rank.
 template <typename T, int kThreads, int kVecs, typename Emit>
 __device__ __forceinline__ void best_columns(RowTile<T, kThreads, kVecs>& tile, float thread_max,
                                              const T* x, int len, int first_column, int n_top,

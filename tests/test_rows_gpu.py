@@ -499,6 +499,29 @@ def test_more_rows_than_one_grid_counts(B):
     assert torch.all((grad.double() - (lp.exp() - hot)).abs() <= tol)
 
 
+@pytest.mark.parametrize("cols", [200, 3001, 40001])
+def test_logits_past_32_bits(B, cols):
+    """Rows whose offsets pass 2^31 elements give what the same rows close
+    together give; a gradient written in place leaves the space between."""
+    n, ld = 5, 600_000_000
+    near = torch.empty(n, cols + 8 - cols % 8, device="cuda", dtype=torch.bfloat16)[:, :cols]
+    near.copy_(torch.randn(n, cols, generator=_gen(cols), device="cuda"))
+    room = torch.empty((n - 1) * ld + cols + 1, device="cuda", dtype=torch.bfloat16)
+    far = room.as_strided((n, cols), (ld, 1))
+    far.copy_(near)
+    room.as_strided((n,), (ld,), cols).fill_(7.0)
+    ids, t, lse = _teacher(near, 5, 1.0, _gen(2))
+    one, two = B.log_probs(near, ids, 4), B.log_probs(far, ids, 4)
+    room_near = torch.empty(n, near.stride(0), device="cuda", dtype=torch.bfloat16)
+    loss, grad = B.distill_loss(near, ids, t, 1.0, lse, grad_out=room_near[:, :cols])
+    loss2, grad2 = B.distill_loss(far, ids, t, 1.0, lse, grad_out=far)
+    torch.cuda.synchronize()
+    for a, b in zip(one, two):
+        assert torch.equal(a, b)
+    assert torch.equal(loss, loss2) and torch.equal(grad, grad2)
+    assert grad2.data_ptr() == far.data_ptr() and torch.all(room.as_strided((n,), (ld,), cols) == 7)
+
+
 def test_empty_batches(B):
     x = torch.empty(0, 7, device="cuda")
     ids = torch.empty(0, 2, device="cuda", dtype=torch.int32)
