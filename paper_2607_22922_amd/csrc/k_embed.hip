@@ -688,6 +688,7 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 // clear_bytes: of the table's gradient (0: needs the most workspace).
 EmbedPlan embed_plan(int64_t rows, int dim, int64_t slots, int64_t clear_bytes) {
   EmbedPlan p{};
+  if (slots == 0) return p;                           // nothing to sort: the table is cleared at most
   int bits = 1;
   while ((rows >> bits) != 0) ++bits;                 // `rows` itself is a key
   int own = 6;

@@ -1,0 +1,31 @@
+"""Row operators on the GPU at the edges of what they accept, against their
+64-bit definitions: empty batches, logits far from 0, ties behind ragged ends,
+rows and teachers without a distribution, narrow ids.  Tolerances are those of
+test_rows_gpu.py."""
+import pytest
+import torch
+
+from tests._gpu_util import say
+from tests.test_rows_gpu import INF, TYPES, _check_distill, _check_log_probs, _gen, _row_view, _teacher
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2607_22922_amd import ifvs
+    return ifvs
+
+
+@pytest.mark.parametrize("rows", [(1 << 19) - 1, 1 << 19, (1 << 20) + 3])
+def test_gradient_of_no_slots_clears_large_tables(B, rows):
+    out = torch.full((rows, 9), 3.0, device="cuda")
+    B.embed_gradient(torch.empty(0, 9, device="cuda"), torch.empty(0, 2, device="cuda", dtype=torch.int32), rows,
+                     out=out)
+    torch.cuda.synchronize()
+    assert torch.all(out == 0)
+    out.fill_(3.0)
+    B.embed_gradient(torch.empty(0, 9, device="cuda"), torch.empty(0, 2, device="cuda", dtype=torch.int32), rows,
+                     out=out, accumulate=True)
+    torch.cuda.synchronize()
+    assert torch.all(out == 3)
