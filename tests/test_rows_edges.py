@@ -20,3 +20,22 @@ def _run(code):
 def test_gradient_workspace_of_an_empty_batch():
     out = _run(f"print([lib.ifvs_embed_workspace(r, 64, 0, bag) for r in {ROWS} for bag in (1, 16)])")
     assert out.strip() == str([0] * 6)
+
+
+@pytest.mark.parametrize("fn", ["ifvs_log_probs_workspace(0, {}, 5)", "ifvs_distill_workspace(0, {})"])
+def test_row_workspaces_of_an_empty_batch(fn):
+    out = _run("print([" + ", ".join("lib." + fn.format(c) for c in COLS) + "])")
+    assert out.strip() == str([0] * len(COLS))
+
+
+def test_empty_batches_of_long_rows_do_nothing():
+    """The whole calls, with nothing to read: NULL arrays and no workspace."""
+    out = _run("""
+import ctypes
+f = ctypes.c_float(1.0)
+for cols in (16385, 131072, 1 << 20):
+    print(lib.ifvs_log_probs(0, cols, None, cols, 1, None, f, None, 1, 5, None, None, None, None, None, 0, None),
+          lib.ifvs_distill_loss(0, cols, None, cols, 1, None, 3, None, None, None, f, None, None, None, cols, None, 0,
+                                None))
+""")
+    assert out.split() == ["0"] * 6

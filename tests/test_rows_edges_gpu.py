@@ -29,3 +29,12 @@ def test_gradient_of_no_slots_clears_large_tables(B, rows):
                      out=out, accumulate=True)
     torch.cuda.synchronize()
     assert torch.all(out == 3)
+
+
+@pytest.mark.parametrize("cols", [1, 16385, 131072, 1 << 20])
+def test_empty_batches_of_long_rows(B, cols):
+    x = torch.empty(0, cols, device="cuda")
+    ids = torch.empty(0, 2, device="cuda", dtype=torch.int32)
+    assert [tuple(o.shape) for o in B.log_probs(x, ids, 4)] == [(0, 2), (0,), (0, 4), (0, 4)]
+    loss, grad = B.distill_loss(x, ids, torch.empty(0, 2, device="cuda"))
+    assert loss.shape == (0,) and grad.shape == (0, cols)
