@@ -222,15 +222,14 @@ struct RowTile {
     if (static_cast<int>(threadIdx.x) < nedge) f(elem_load(x + edge_column()), edge_column());
   }
 
-  // The same a vector a load, columns ascending but for the edge's, until f
-  // returns false.
+  // The same a vector a load, columns ascending (an edge before the vectors, or
+  // the one after them), until f returns false.  f sees all of a vector.
   template <typename F>
   __device__ __forceinline__ void each_vector_from_memory(const T* x, F&& f) const {
     const int tid = threadIdx.x;
-    if (tid < nedge && !f(elem_load(x + edge_column()), edge_column()) && tid < head) return;
+    if (tid < head && !f(elem_load(x + tid), tid)) return;
 #pragma unroll 1
-    for (int i = 0; i < kVecs; ++i) {
-      if (tid >= nvec - i * kThreads) return;
+    for (int i = 0; i < kVecs && tid < nvec - i * kThreads; ++i) {
       float y[kE];
       Elem<T>::unpack(load_words_again(x + column(i, 0)), y);
       bool more = true;
@@ -238,6 +237,7 @@ struct RowTile {
       for (int j = 0; j < kE; ++j) more = f(y[j], column(i, j)) && more;
       if (!more) return;
     }
+    if (tid >= head && tid < nedge) f(elem_load(x + edge_column()), edge_column());
   }
 
   // Between two passes over the tile: the compiler would keep every unpacked

@@ -38,3 +38,32 @@ def test_empty_batches_of_long_rows(B, cols):
     assert [tuple(o.shape) for o in B.log_probs(x, ids, 4)] == [(0, 2), (0,), (0, 4), (0, 4)]
     loss, grad = B.distill_loss(x, ids, torch.empty(0, 2, device="cuda"))
     assert loss.shape == (0,) and grad.shape == (0, cols)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [2001, 2047, 4091, 16383, 35003, 40001])
+def test_alternatives_of_ties_with_ragged_ends(B, dtype, cols):
+    """Long ties behind a lower or masked start, at every alignment: a row's
+    first and last elements lie outside its whole vectors."""
+    say(f"[ragged ties] {dtype} cols={cols}")
+    leads = [l for l in (1, 255, 256, 512, 1024, 2048, 8200, 20000) if l < cols - 1100]
+    for shift in range(8):
+        x = torch.zeros(2 * len(leads) * (cols + 3) + shift, device="cuda", dtype=dtype)
+        x = x[shift:].view(2 * len(leads), cols + 3)[:, :cols]
+        for i, lead in enumerate(leads):
+            x[2 * i, :lead] = -1.0
+            x[2 * i + 1, :lead] = -INF
+        _check_log_probs(B, x, 1.0, None, None, 10 if shift % 2 else 32)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shift", [0, 3])
+def test_alternatives_of_ties_in_ragged_chunks(B, dtype, shift):
+    """The same in rows of many chunks of 16384 columns: the tie starts in a
+    later round of its chunk, at the threads that hold the chunk's ends."""
+    say(f"[ragged ties in chunks] {dtype} shift={shift}")
+    cols = (1 << 20) - 5
+    x = torch.zeros(2 * cols + shift, device="cuda", dtype=dtype)[shift:].view(2, cols)
+    x[0, :30 * 16384 + 8192] = -1.0
+    x[1, :47 * 16384 + 4096] = -1.0
+    _check_log_probs(B, x, 1.0, None, None, 10)
