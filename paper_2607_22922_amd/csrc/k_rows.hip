@@ -8,9 +8,10 @@
 // only rounding is that of the small exponent, so rows far from 0 lose
 // nothing, and sums with different references join by exact powers of two.
 // Then S = sum e_v, log2 q_v = x_v c - b - log2 S, and the entropy is
-// log S - (sum e_v (x_v c - b)) ln 2 / S: every term has one sign.  Where
-// max(x) c passes 1e37 (rows masked throughout with the lowest value) two
-// different logits lie so far apart that e_v is 1 at the maximum, else 0.
+// log S - (sum e_v (x_v c - b)) ln 2 / S: every term has one sign.  From
+// |max(x) c| = 2^24 on (columns masked throughout with a finite value, a small
+// tau) fp32 does not hold every whole number: b and the exponents are computed
+// in 64 bits there, which a wavefront decides for its columns.
 //
 // A workgroup holds its piece of a row in registers, so a row is read once
 // whatever is computed from it: maximum, sums, the best columns, and in the
@@ -30,6 +31,7 @@ namespace {
 
 constexpr double kLn2 = 0.69314718055994530942;
 constexpr float kExpFloor = -200.0f;            // 2^-200 is 0 in fp32
+constexpr float kFar = 16777216.0f;             // 2^24: fp32 holds every whole number below
 constexpr float kHuge = 1e37f;
 constexpr int kMaxChunks = 64;                  // one per lane of the joining wavefront; 2^20 fp32 columns are 64
 static_assert(IFVS_MAX_COLS / 4 <= kMaxChunks * 4096, "chunks of 4096 vectors");
@@ -42,6 +44,13 @@ __device__ __forceinline__ float exp2_fast(float z) { return __builtin_amdgcn_ex
 
 __device__ __forceinline__ double times_pow2(double v, double e) {
   return ldexp(v, static_cast<int>(fmax(fmin(e, 4000.0), -4000.0)));
+}
+
+// x c - origin for a whole origin near the maximum's x c, far from 0.  (Equal
+// logits have equal products; where a product is rounded, past 2^53, others
+// lie thousands of powers of two apart.)
+__device__ __forceinline__ float far_exponent(float x, double c, double origin) {
+  return static_cast<float>(static_cast<double>(x) * c - origin);
 }
 
 __device__ __forceinline__ int row_cols(const int32_t* n_valid, int64_t i, int64_t cols) {
@@ -79,37 +88,35 @@ __device__ __forceinline__ Stat join_lanes(const Stat& mine) {
 }
 
 // The sums of a wavefront's elements, in every lane.
-template <bool kEntropy, typename T, int kThreads, int kVecs>
-__device__ __forceinline__ Stat wave_stat(RowTile<T, kThreads, kVecs>& tile, const T* x, float mx, float c) {
+template <typename T, int kThreads, int kVecs>
+__device__ __forceinline__ Stat wave_stat(RowTile<T, kThreads, kVecs>& tile, float mx, float c) {
   constexpr int kE = Elem<T>::kPerVec;
   tile.forget_unpacked();
   float sum = 0.0f, wsum = 0.0f;
-  double origin = 0.0;
   const float b = mx == -INFINITY ? 0.0f : rintf(mx * c);
-  if (fabsf(b) < kHuge) {
-    origin = b;
-    auto add = [&](float v) {
-      const float z = __fmaf_rn(v, c, -b);
-      const float e = exp2_fast(z);
-      sum += e;
-      if constexpr (kEntropy) wsum = __fmaf_rn(e, fmaxf(z, kExpFloor), wsum);
-    };
+  double origin = b;
+  auto add = [&](float z) {
+    const float e = exp2_fast(z);
+    sum += e;
+    wsum = __fmaf_rn(e, fmaxf(z, kExpFloor), wsum);
+  };
+  if (fabsf(b) < kFar) {
 #pragma unroll
     for (int i = 0; i < kVecs; ++i)
       if (tile.has(i)) {
         float f[kE];
         Elem<T>::unpack(tile.v[i], f);
 #pragma unroll
-        for (int j = 0; j < kE; ++j) add(f[j]);
+        for (int j = 0; j < kE; ++j) add(__fmaf_rn(f[j], c, -b));
         __builtin_amdgcn_sched_barrier(0);
       }
-    add(tile.edge);
+    add(__fmaf_rn(tile.edge, c, -b));
   } else {
-    origin = static_cast<double>(mx) * c;
-    tile.each_from_memory(x, [&](float v, int) { sum += v == mx ? 1.0f : (isnan(v) ? NAN : 0.0f); });
-    if (mx == INFINITY) sum = NAN;
+    const double wide = c;                          // its products with a logit are exact
+    origin = rint(mx * wide);
+    tile.each([&](float v, int) { add(far_exponent(v, wide, origin)); });
   }
-  return {origin, wave_add(static_cast<double>(sum)), kEntropy ? wave_add(static_cast<double>(wsum)) : 0.0};
+  return {origin, wave_add(static_cast<double>(sum)), wave_add(static_cast<double>(wsum))};
 }
 
 // ------------------------------------------------------------ best columns
@@ -382,7 +389,7 @@ __global__ __launch_bounds__(kThreads, 4) void log_probs_tile_kernel(const LogPr
   RowTile<T, kThreads, kVecs> tile;
   tile.load(x + first, mine);
   const float tmax = tile.thread_max();
-  Stat st = wave_stat<true>(tile, x + first, wave_max(tmax), static_cast<float>(a.c));
+  Stat st = wave_stat(tile, wave_max(tmax), static_cast<float>(a.c));
   if constexpr (kWaves > 1) {
     if ((tid & 63) == 0) s_stat[wave] = st;
     __syncthreads();

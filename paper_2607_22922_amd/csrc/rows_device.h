@@ -222,7 +222,22 @@ struct RowTile {
     if (static_cast<int>(threadIdx.x) < nedge) f(elem_load(x + edge_column()), edge_column());
   }
 
-  // The same a vector a load, columns ascending (an edge before the vectors, or
+  // The thread's elements one by one: f(x, column).
+  template <typename F>
+  __device__ __forceinline__ void each(F&& f) const {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i)
+      if (static_cast<int>(threadIdx.x) < nvec - i * kThreads) {
+        float y[kE];
+        Elem<T>::unpack(v[i], y);
+#pragma unroll
+        for (int j = 0; j < kE; ++j) f(y[j], column(i, j));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    if (static_cast<int>(threadIdx.x) < nedge) f(edge, edge_column());
+  }
+
+  // From memory, a vector a load, columns ascending (an edge before the vectors, or
   // the one after them), until f returns false.  f sees all of a vector.
   template <typename F>
   __device__ __forceinline__ void each_vector_from_memory(const T* x, F&& f) const {

@@ -67,3 +67,41 @@ def test_alternatives_of_ties_in_ragged_chunks(B, dtype, shift):
     x[0, :30 * 16384 + 8192] = -1.0
     x[1, :47 * 16384 + 4096] = -1.0
     _check_log_probs(B, x, 1.0, None, None, 10)
+
+
+def _far_rows(dtype, cols, n, seed):
+    """Rows with finite masks far below 0 (whole rows, a stretch that fills
+    wavefronts and chunks, every other column, all columns but one), rows far
+    from 0 on either side and rows of large logits of both signs.  fp16 holds
+    what it can (65504)."""
+    masks = [-1e9, -1e10, -1e12, -1e20, -1e30] if dtype != torch.float16 else [-6e4, -6.5e4]
+    x = _row_view(n, cols, dtype, _gen(seed))
+    i = 0
+    for m in masks:
+        x[i] = m
+        x[i + 1, cols // 8:cols - cols // 8] = m
+        x[i + 2, ::2] = m
+        x[i + 3, :] = m
+        x[i + 3, cols // 3] = 0.5
+        i += 4
+    for far in (1e10, -3e15) if dtype != torch.float16 else (6e4, -3e4):
+        x[i] = far
+        x[i + 1] = x[i + 1].float() * (abs(far) / 16.0)
+        i += 2
+    return x, i
+
+
+FAR_ROWS = 24
+# 1 / tau large takes ordinary logits as far (fp16 masks reach 2^30 at 1e-4)
+FAR_TAUS = [1.0, 1e-4, 1e-6, 1e-9]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tau", FAR_TAUS)
+@pytest.mark.parametrize("cols", [50, 3001, 40001])
+def test_log_probs_far_from_zero(B, dtype, tau, cols):
+    say(f"[far logprobs] {dtype} tau={tau} cols={cols}")
+    x, _ = _far_rows(dtype, cols, FAR_ROWS, cols)
+    given = torch.tensor([[0, cols // 2, cols - 1, -1, cols // 3]], device="cuda",
+                         dtype=torch.int32).repeat(FAR_ROWS, 1)
+    _check_log_probs(B, x, tau, None, given, 12)
