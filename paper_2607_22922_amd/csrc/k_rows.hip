@@ -32,7 +32,6 @@ namespace {
 constexpr double kLn2 = 0.69314718055994530942;
 constexpr float kExpFloor = -200.0f;            // 2^-200 is 0 in fp32
 constexpr float kFar = 16777216.0f;             // 2^24: fp32 holds every whole number below
-constexpr float kHuge = 1e37f;
 constexpr int kMaxChunks = 64;                  // one per lane of the joining wavefront; 2^20 fp32 columns are 64
 static_assert(IFVS_MAX_COLS / 4 <= kMaxChunks * 4096, "chunks of 4096 vectors");
 constexpr int64_t kMaxGrid = 1 << 22;           // workgroups of one launch
@@ -697,16 +696,15 @@ __device__ __forceinline__ DistillEnd distill_end(const DistillArgs& a, const Di
 
 // The other columns' sum in a wavefront's registers, in every lane.
 template <typename T, int kThreads, int kVecs>
-__device__ __forceinline__ Stat other_stat(RowTile<T, kThreads, kVecs>& tile, const T* x, const unsigned char* bits,
-                                           float mx, const DistillArgs& a) {
+__device__ __forceinline__ Stat other_stat(RowTile<T, kThreads, kVecs>& tile, float mx, const DistillArgs& a) {
   constexpr int kE = Elem<T>::kPerVec;
   const SplitC c = split_c(a.c);
   const float b = mx == -INFINITY ? 0.0f : rintf(mx * c.hi);
   float sum = 0.0f;
   double origin = b;
-  if (fabsf(b) < kHuge) {
+  tile.forget_unpacked();
+  if (fabsf(b) < kFar) {
     auto add = [&](float v) { sum += exp2_fast(__fmaf_rn(v, c.lo, __fmaf_rn(v, c.hi, -b))); };
-    tile.forget_unpacked();
 #pragma unroll
     for (int i = 0; i < kVecs; ++i)
       if (tile.has(i)) {
@@ -718,13 +716,8 @@ __device__ __forceinline__ Stat other_stat(RowTile<T, kThreads, kVecs>& tile, co
       }
     add(tile.edge);
   } else {
-    origin = mx * a.c;
-    tile.each_from_memory(x, [&](float v, int column) {
-      const int bit = tile.bit_of(column);
-      if ((bits[bit >> 3] >> (bit & 7)) & 1u) return;
-      sum += v == mx ? 1.0f : (isnan(v) ? NAN : 0.0f);
-    });
-    if (mx == INFINITY) sum = NAN;
+    origin = rint(mx * a.c);
+    tile.each([&](float v, int) { sum += exp2_fast(far_exponent(v, a.c, origin)); });
   }
   return {origin, wave_add(static_cast<double>(sum)), 0.0};
 }
@@ -750,13 +743,15 @@ __device__ __forceinline__ void write_others(RowTile<T, kThreads, kVecs>& tile, 
   const int tid = threadIdx.x;
   const SplitC c = split_c(a.c);
   const float coef = r.coef;
-  if (fabs(r.origin) >= kHuge) {
-    tile.each_from_memory(x, [&](float v, int column) { grad[column] = elem_round<T>(v * a.c == r.origin ? coef : 0.0f); });
+  tile.forget_unpacked();
+  if (!(fabs(r.origin) < kFar)) {
+    tile.each_from_memory(x, [&](float v, int column) {
+      grad[column] = elem_round<T>(coef * exp2_fast(far_exponent(v, a.c, r.origin)));
+    });
     return;
   }
   const float b = static_cast<float>(r.origin);
   auto gradient = [&](float v) { return coef * exp2_fast(__fmaf_rn(v, c.lo, __fmaf_rn(v, c.hi, -b))); };
-  tile.forget_unpacked();
 #pragma unroll
   for (int i = 0; i < kVecs; ++i)
     if (tile.has(i)) {
@@ -941,7 +936,7 @@ __global__ __launch_bounds__(kThreads, 4) void distill_tile_kernel(const Distill
   if (kTeacherFirst) tile.load(x, mine);
   group_sync<kThreads>();
   drop_named(tile, t.bits);
-  const Stat other = other_stat(tile, x, t.bits, wave_max(tile.thread_max()), a);
+  const Stat other = other_stat(tile, wave_max(tile.thread_max()), a);
   join_row<kThreads>(a, weight, other, s_stat, s_teacher, kWhole ? &s_row : nullptr);
   if constexpr (kWhole) {
     const DistillRow r = s_row;
@@ -988,7 +983,7 @@ __global__ __launch_bounds__(kThreads) void distill_long_kernel(const DistillArg
     if (tid < 64) mark_named(tile, a, t, at, n);
     __syncthreads();
     drop_named(tile, t.bits);
-    other = join(other, other_stat(tile, x + at, t.bits, wave_max(tile.thread_max()), a));
+    other = join(other, other_stat(tile, wave_max(tile.thread_max()), a));
     if (at == 0) break;
     __syncthreads();                                   // the segment's bits have been read
   }

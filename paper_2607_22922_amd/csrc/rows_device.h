@@ -210,18 +210,6 @@ struct RowTile {
     return kThreads * kVecs * 8 + (in < 0 ? column : column - nvec * kE);
   }
 
-  // The thread's elements one by one from memory, for rare paths that must not
-  // cost the others registers: f(x, column).
-  template <typename F>
-  __device__ __forceinline__ void each_from_memory(const T* x, F&& f) const {
-#pragma unroll 1
-    for (int i = 0; i < kVecs; ++i)
-      if (static_cast<int>(threadIdx.x) < nvec - i * kThreads)
-#pragma unroll 1
-        for (int j = 0; j < kE; ++j) f(elem_load(x + column(i, j)), column(i, j));
-    if (static_cast<int>(threadIdx.x) < nedge) f(elem_load(x + edge_column()), edge_column());
-  }
-
   // The thread's elements one by one: f(x, column).
   template <typename F>
   __device__ __forceinline__ void each(F&& f) const {
@@ -237,7 +225,19 @@ struct RowTile {
     if (static_cast<int>(threadIdx.x) < nedge) f(edge, edge_column());
   }
 
-  // From memory, a vector a load, columns ascending (an edge before the vectors, or
+  // The same from memory, for rare paths that must not cost the others
+  // registers.
+  template <typename F>
+  __device__ __forceinline__ void each_from_memory(const T* x, F&& f) const {
+#pragma unroll 1
+    for (int i = 0; i < kVecs; ++i)
+      if (static_cast<int>(threadIdx.x) < nvec - i * kThreads)
+#pragma unroll 1
+        for (int j = 0; j < kE; ++j) f(elem_load(x + column(i, j)), column(i, j));
+    if (static_cast<int>(threadIdx.x) < nedge) f(elem_load(x + edge_column()), edge_column());
+  }
+
+  // The same a vector a load, columns ascending (an edge before the vectors, or
   // the one after them), until f returns false.  f sees all of a vector.
   template <typename F>
   __device__ __forceinline__ void each_vector_from_memory(const T* x, F&& f) const {

@@ -105,3 +105,24 @@ def test_log_probs_far_from_zero(B, dtype, tau, cols):
     given = torch.tensor([[0, cols // 2, cols - 1, -1, cols // 3]], device="cuda",
                          dtype=torch.int32).repeat(FAR_ROWS, 1)
     _check_log_probs(B, x, tau, None, given, 12)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("tau", [1.0, 1e-4, 1e-9])
+@pytest.mark.parametrize("cols,n", [(50, 28), (3001, 28), (40001, 28), (40001, 131), (9001, 514)])
+def test_distill_far_from_zero(B, dtype, rest, tau, cols, n):
+    """The far columns are others, named ones, or both; named ones of ordinary
+    size among others that are all far below."""
+    say(f"[far distill] {dtype} tau={tau} cols={cols} n={n} rest={rest}")
+    x, far = _far_rows(dtype, cols, n, cols)
+    gen = _gen(cols + 1)
+    ids = torch.rand(n, cols, generator=gen, device="cuda").topk(6, 1).indices.to(torch.int32)
+    t = tau * torch.randn(n, 6, generator=gen, device="cuda")
+    # a teacher that takes some half of its probability to the named columns
+    lse = torch.logsumexp(t / tau, 1) + 0.7
+    x[0, ids[0].long()] = torch.randn(6, generator=gen, device="cuda").to(dtype)
+    if dtype != torch.float16:
+        x[4, ids[4].long()] = torch.randn(6, generator=gen, device="cuda").to(dtype)
+    weight = torch.rand(n, generator=gen, device="cuda") + 0.5
+    _check_distill(B, x, ids, t, tau, lse if rest else None, weight)
