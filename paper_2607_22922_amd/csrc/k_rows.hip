@@ -541,7 +541,7 @@ __device__ __forceinline__ TeacherLds teacher_lds(unsigned char* smem, int n_tea
 
 // What one wavefront finds out about the teacher.
 struct Teacher {
-  double lse;          // natural logarithm of its sum
+  double top, lse;     // log p = (t - top) / tau - lse: the largest logit apart, which may be 1e38
   double rest;         // P
   bool bad, present;
   bool repeats;        // two slots name one column of the chunk
@@ -586,6 +586,7 @@ __device__ __forceinline__ Teacher read_teacher(const DistillArgs& a, int64_t ro
   out.present = __any(present);
   mx = wave_max(mx);
   if (a.teacher_lse) {
+    out.top = 0.0;
     out.lse = a.teacher_lse[row];
     if (!isfinite(out.lse)) bad = true;
   } else {
@@ -593,11 +594,12 @@ __device__ __forceinline__ Teacher read_teacher(const DistillArgs& a, int64_t ro
     double sum = 0.0;
     for (int k = lane; k < a.n_teacher; k += 64)
       if (ids[k] >= 0 && ids[k] < len) sum += exp((static_cast<double>(logits[k]) - mx) * inv_tau);
-    out.lse = mx * inv_tau + log(wave_add(sum));
+    out.top = mx;
+    out.lse = log(wave_add(sum));
   }
   double psum = 0.0;
   for (int k = lane; k < a.n_teacher; k += 64) {
-    const double p = ids[k] >= 0 && ids[k] < len ? exp(logits[k] * inv_tau - out.lse) : 0.0;
+    const double p = ids[k] >= 0 && ids[k] < len ? exp((logits[k] - out.top) * inv_tau - out.lse) : 0.0;
     t.p[k] = p;
     psum += p;
   }
@@ -636,7 +638,7 @@ __device__ __forceinline__ DistillStat named_stat(const DistillArgs& a, int64_t 
       for (int o = 0; o < k; ++o) again |= t.column[o] == column;
     if (!again) sum += pow2(z);
     if (p > 0.0) {
-      loss += p * (logits[k] * inv_tau - teacher.lse - z * kLn2);
+      loss += p * ((logits[k] - teacher.top) * inv_tau - teacher.lse - z * kLn2);
       psum += p;
     }
   }

@@ -126,3 +126,20 @@ def test_distill_far_from_zero(B, dtype, rest, tau, cols, n):
         x[4, ids[4].long()] = torch.randn(6, generator=gen, device="cuda").to(dtype)
     weight = torch.rand(n, generator=gen, device="cuda") + 0.5
     _check_distill(B, x, ids, t, tau, lse if rest else None, weight)
+
+
+@pytest.mark.parametrize("cols,n", [(50, 9), (3001, 9), (40001, 9), (40001, 131)])
+def test_distill_of_teachers_far_from_zero(B, cols, n):
+    """A teacher whose logits are all masked with one finite value follows a
+    uniform distribution over its slots; distances of any size are teachers."""
+    say(f"[far teacher] cols={cols} n={n}")
+    gen = _gen(cols)
+    x = _row_view(n, cols, torch.float32, gen)
+    ids, t, _ = _teacher(x, 6, 1.0, gen)
+    low = torch.finfo(torch.float32).min
+    for i, far in enumerate((low, -1e30, -1e20, -1e17, 1e16, 3e38)):
+        t[i] = far
+    t[6, :3] = low
+    t[7] = 1e15 + torch.arange(6, device="cuda") * 6.7e7          # steps of one fp32 unit
+    _check_distill(B, x, ids, t, 1.0)
+    _check_distill(B, x, ids, t, 3.0)
