@@ -567,9 +567,11 @@ int64_t ifvs_distill_workspace(int64_t n, int64_t cols);
  * grad_out = row_weight[i] * dL/dz, rounded once, and 0 in the columns from
  * n_valid[i] on.  A row of weight 0 is left out: loss 0, gradient 0, nothing
  * of it read.  So is a row that has no present slot and no teacher_lse, or no
- * column above -inf.  A NaN or +inf among a row's logits or its present
- * teacher logits makes its loss and gradient NaN, and so do, without
- * teacher_lse, present teacher logits that are all -inf.
+ * column above -inf (a padding row, whatever its teacher_lse).  A NaN or +inf
+ * among a row's logits or its present teacher logits makes its loss and
+ * gradient NaN, and so does, in a row that is not left out, a teacher without
+ * a distribution: a teacher_lse that is not finite or, without teacher_lse,
+ * present teacher logits that are all -inf.
  *  logits: device [n] rows of cols elements of type dtype, ld apart
  *  n_valid: device [n] int32 (clamped to 0..cols), or NULL
  *  teacher_ids: device [n][n_teacher] int32; teacher_logits: device

@@ -543,7 +543,8 @@ __device__ __forceinline__ TeacherLds teacher_lds(unsigned char* smem, int n_tea
 struct Teacher {
   double top, lse;     // log p = (t - top) / tau - lse: the largest logit apart, which may be 1e38
   double rest;         // P
-  bool bad, present;
+  bool bad, present;   // a NaN or +inf among the present slots; any
+  bool undefined;      // its sum has no logarithm (rows left out do not look at it)
   bool repeats;        // two slots name one column of the chunk
 };
 
@@ -588,9 +589,9 @@ __device__ __forceinline__ Teacher read_teacher(const DistillArgs& a, int64_t ro
   if (a.teacher_lse) {
     out.top = 0.0;
     out.lse = a.teacher_lse[row];
-    if (!isfinite(out.lse)) bad = true;
+    out.undefined = !isfinite(out.lse);
   } else {
-    if (out.present && mx == -INFINITY) bad = true;
+    out.undefined = out.present && mx == -INFINITY;
     double sum = 0.0;
     for (int k = lane; k < a.n_teacher; k += 64)
       if (ids[k] >= 0 && ids[k] < len) sum += exp((static_cast<double>(logits[k]) - mx) * inv_tau);
@@ -672,6 +673,10 @@ __device__ __forceinline__ DistillRow distill_row(const DistillArgs& a, const Di
     return r;
   }
   if (!other && !named) return r;                                     // no distribution
+  if (teacher.undefined) {
+    r.mode = kRowNan;
+    return r;
+  }
   r.hi = fmax(other ? st.other_origin : -INFINITY, named ? st.named_origin : -INFINITY);
   const double others = other ? times_pow2(st.other_sum, st.other_origin - r.hi) : 0.0;
   r.all = others + (named ? times_pow2(st.named_sum, st.named_origin - r.hi) : 0.0);

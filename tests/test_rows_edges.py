@@ -3,7 +3,10 @@ of empty batches, and the definitions' answers for rows without a distribution."
 import subprocess
 import sys
 
+import numpy as np
 import pytest
+
+from oracle import ifvs_rows_oracle as R
 
 ROWS = [(1 << 19) - 1, 1 << 19, (1 << 31) - 2]
 COLS = [1, 16384, 16385, 131072, 1 << 20]
@@ -39,3 +42,19 @@ for cols in (16385, 131072, 1 << 20):
                                 None))
 """)
     assert out.split() == ["0"] * 6
+
+
+@pytest.mark.parametrize("with_lse", [False, True])
+def test_definition_leaves_out_rows_without_a_distribution(with_lse):
+    """A padding row's teacher has no distribution either (its logits are all
+    -inf, its sum's logarithm -inf or undefined): loss and gradient stay 0.  A
+    NaN among the row's present teacher logits shows, and so does an undefined
+    sum beside a student that has a distribution."""
+    x = np.full((5, 6), -np.inf)
+    x[4] = np.arange(6)
+    ids = np.tile([1, 3], (5, 1))
+    t = np.array([[-np.inf, -np.inf], [-np.inf, -np.inf], [0.5, 1.0], [np.nan, 1.0], [0.5, 1.0]])
+    lse = np.array([-np.inf, np.nan, np.inf, 0.0, -np.inf])
+    loss, grad = R.distill(x, ids, t, teacher_lse=lse if with_lse else None)
+    assert np.all(loss[:3] == 0) and np.all(grad[:3] == 0)
+    assert np.isnan(loss[3]) and np.isnan(loss[4]) == with_lse

@@ -143,3 +143,28 @@ def test_distill_of_teachers_far_from_zero(B, cols, n):
     t[7] = 1e15 + torch.arange(6, device="cuda") * 6.7e7          # steps of one fp32 unit
     _check_distill(B, x, ids, t, 1.0)
     _check_distill(B, x, ids, t, 3.0)
+
+
+@pytest.mark.parametrize("cols,n", [(50, 8), (3001, 8), (40001, 8), (40001, 131)])
+@pytest.mark.parametrize("rest", [False, True])
+def test_distill_leaves_out_padding_rows(B, rest, cols, n):
+    """Rows without a column above -inf, as a padded batch holds them, are left
+    out whatever their teacher's sum is; a row with a distribution is not, and
+    NaN among teacher logits shows."""
+    say(f"[padding rows] cols={cols} n={n} rest={rest}")
+    gen = _gen(cols)
+    x = _row_view(n, cols, torch.float32, gen)
+    ids, t, lse = _teacher(x, 6, 1.0, gen)
+    n_valid = torch.full((n,), cols, device="cuda", dtype=torch.int32)
+    n_valid[0] = n_valid[1] = 0
+    lse[0], lse[1] = -INF, float("nan")
+    x[2:5] = -INF
+    t[2:4] = -INF
+    lse[2], lse[3] = -INF, INF
+    t[4, 1] = float("nan")
+    lse[5] = -INF
+    loss, grad = B.distill_loss(x, ids, t, 1.0, lse if rest else None, None, n_valid)
+    torch.cuda.synchronize()
+    assert torch.all(loss[:4] == 0) and torch.all(grad[:4] == 0)
+    assert bool(torch.isnan(loss[4])) and bool(torch.isnan(loss[5])) == rest
+    _check_distill(B, x, ids, t, 1.0, lse if rest else None, None, n_valid)
