@@ -596,6 +596,9 @@ def _ld(t):
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
+_NARROW = (torch.int8, torch.uint8, torch.int16, torch.uint16)       # every value fits 32 bits
+
+
 def _small_arg(t, name, dtype, shape, device):
     """A contiguous tensor of `dtype` and `shape` on `device` (None stays None)."""
     if t is None:
@@ -606,7 +609,8 @@ def _small_arg(t, name, dtype, shape, device):
         if dtype == torch.int32:
             if t.is_floating_point() or t.is_complex() or t.dtype == torch.bool:
                 raise IfvsError(E_INVALID, f"{name} must be whole numbers")
-            t = t.clamp(-1, 0x7FFFFFFF)          # numbers past 32 bits must not wrap into range
+            if t.dtype not in _NARROW:           # numbers past 32 bits must not wrap into range
+                t = t.to(torch.int64).clamp(-1, 0x7FFFFFFF)
         t = t.to(dtype)
     return t if t.is_contiguous() else t.contiguous()
 

@@ -5,8 +5,10 @@ import sys
 
 import numpy as np
 import pytest
+import torch
 
 from oracle import ifvs_rows_oracle as R
+from paper_2607_22922_amd import ifvs
 
 ROWS = [(1 << 19) - 1, 1 << 19, (1 << 31) - 2]
 COLS = [1, 16384, 16385, 131072, 1 << 20]
@@ -58,3 +60,21 @@ def test_definition_leaves_out_rows_without_a_distribution(with_lse):
     loss, grad = R.distill(x, ids, t, teacher_lse=lse if with_lse else None)
     assert np.all(loss[:3] == 0) and np.all(grad[:3] == 0)
     assert np.isnan(loss[3]) and np.isnan(loss[4]) == with_lse
+
+
+@pytest.mark.parametrize("wide,values,want", [
+    (torch.int8, [-128, -1, 127], [-128, -1, 127]), (torch.uint8, [0, 255], [0, 255]),
+    (torch.int16, [-32768, 32767], [-32768, 32767]), (torch.uint16, [0, 65535], [0, 65535]),
+    (torch.uint32, [7, 2**32 - 1], [7, 2**31 - 1]), (torch.int64, [-2**40, 3, 2**32 + 3], [-1, 3, 2**31 - 1])])
+def test_whole_numbers_become_32_bits(wide, values, want):
+    """Narrow types keep their values; numbers past 32 bits stay outside."""
+    t = torch.tensor(values, dtype=torch.int64).to(wide)
+    got = ifvs._small_arg(t, "ids", torch.int32, (len(values),), t.device)
+    assert got.dtype == torch.int32 and got.tolist() == want
+
+
+@pytest.mark.parametrize("bad", [torch.float32, torch.bool, torch.complex64])
+def test_other_types_are_no_ids(bad):
+    t = torch.zeros(3).to(bad)
+    with pytest.raises(ifvs.IfvsError):
+        ifvs._small_arg(t, "ids", torch.int32, (3,), t.device)

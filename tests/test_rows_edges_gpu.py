@@ -168,3 +168,27 @@ def test_distill_leaves_out_padding_rows(B, rest, cols, n):
     assert torch.all(loss[:4] == 0) and torch.all(grad[:4] == 0)
     assert bool(torch.isnan(loss[4])) and bool(torch.isnan(loss[5])) == rest
     _check_distill(B, x, ids, t, 1.0, lse if rest else None, None, n_valid)
+
+
+@pytest.mark.parametrize("wide", [torch.int8, torch.uint8, torch.int16, torch.uint16, torch.uint32, torch.int64])
+def test_ids_of_any_whole_type(B, wide):
+    """Ids, lengths and slots of every whole-number type name what 32-bit ones
+    name (255 of uint8 is a column, not an absent slot)."""
+    x = torch.randn(6, 300, generator=_gen(1), device="cuda")
+    top = 256 if wide not in (torch.int8,) else 128
+    ids = torch.randint(0, top, (6, 3), generator=_gen(2), device="cuda", dtype=torch.int32)
+    ids[0, 0] = top - 1
+    nv = torch.tensor([100, 120, 5, 77, 1, 90], device="cuda", dtype=torch.int32)
+    t = torch.randn(6, 3, generator=_gen(3), device="cuda")
+    ids2, nv2 = ids.to(wide), nv.to(wide)
+    want = (B.embed_lookup(x, ids.clamp(max=5)), B.embed_gradient(x, ids, 300), *B.log_probs(x, ids, 4, n_valid=nv),
+            *B.log_probs(x, ids, 0)[:2], *B.distill_loss(x, ids, t, n_valid=nv), *B.distill_loss(x, ids, t))
+    got = (B.embed_lookup(x, ids.clamp(max=5).to(wide)), B.embed_gradient(x, ids2, 300),
+           *B.log_probs(x, ids2, 4, n_valid=nv2), *B.log_probs(x, ids2, 0)[:2],
+           *B.distill_loss(x, ids2, t, n_valid=nv2), *B.distill_loss(x, ids2, t))
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a.view(torch.int32), b.view(torch.int32))
+    if wide in (torch.int8, torch.int16, torch.int64):
+        absent = torch.full((6, 1), -1, device="cuda", dtype=wide)
+        assert torch.all(B.embed_lookup(x, absent) == 0) and torch.all(B.log_probs(x, absent)[0] == -INF)
