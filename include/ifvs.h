@@ -428,9 +428,12 @@ ifvs_status ifvs_train_step(ifvs_index* idx, int32_t nq, const float* q, const i
  *  lut: device [nq][m][256] in lut_dtype (from ifvs_build_lut)
  *  cand: device [nq][n_cand] int32 original ids; logits_out: device
  *        [nq][n_cand] fp32
- * Enqueued on `stream`.  On a clustered index the first call allocates n ints.
- * Errors: IFVS_E_STATE (NULL handle), IFVS_E_INVALID (nq, unknown dtype, n_cand
- * outside 1..IFVS_MAX_COLS, NULL arrays), IFVS_E_NOMEM, IFVS_E_HIP. */
+ * Enqueued on `stream`.  On a clustered index the first call (or training step)
+ * allocates n ints and waits until they are filled, so that later calls may run
+ * on any stream.
+ * Errors: IFVS_E_STATE (NULL handle, that first call while `stream` is being
+ * captured), IFVS_E_INVALID (nq, unknown dtype, n_cand outside
+ * 1..IFVS_MAX_COLS, NULL arrays), IFVS_E_NOMEM, IFVS_E_HIP. */
 ifvs_status ifvs_score_candidates(ifvs_index* idx, int32_t nq, const void* lut, int32_t lut_dtype,
                                   const int32_t* cand, int32_t n_cand, float* logits_out, void* stream);
 

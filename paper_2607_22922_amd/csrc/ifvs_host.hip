@@ -2522,16 +2522,24 @@ ifvs_status distill_buffers(ifvs_index* idx, int32_t n_cand) {
   return IFVS_OK;
 }
 
-// Candidates are original ids; the codes are in physical order.
+// Candidates are original ids; the codes are in physical order.  The inverse
+// is made once and waited for, since the next call may run on another stream.
 ifvs_status candidate_rows(ifvs_index* idx, hipStream_t s) {
   if (!idx->perm || idx->inv_perm) return IFVS_OK;
-  if (ifvs_status st = dev_alloc(&idx->inv_perm, static_cast<size_t>(idx->n), "inverse permutation"); st != IFVS_OK)
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  IFVS_HIP(hipStreamIsCapturing(s, &capture), "looking for a capture");
+  if (capture != hipStreamCaptureStatusNone)
+    return fail(IFVS_E_STATE, "the first call with candidates on a clustered index allocates and cannot be captured");
+  int32_t* inverse = nullptr;
+  if (ifvs_status st = dev_alloc(&inverse, static_cast<size_t>(idx->n), "inverse permutation"); st != IFVS_OK)
     return st;
-  if (hipError_t e = launch_invert_perm(idx->perm, idx->n, idx->inv_perm, s); e != hipSuccess) {
-    hipFree(idx->inv_perm);
-    idx->inv_perm = nullptr;
-    return hip_fail(e, "launching permutation inverse");
+  hipError_t e = launch_invert_perm(idx->perm, idx->n, inverse, s);
+  if (e == hipSuccess) e = hipStreamSynchronize(s);
+  if (e != hipSuccess) {
+    (void)hipFree(inverse);
+    return hip_fail(e, "inverting the cluster permutation");
   }
+  idx->inv_perm = inverse;
   return IFVS_OK;
 }
 

@@ -1,0 +1,63 @@
+"""Scores of listed candidates as callers may use them: several streams,
+captured graphs, candidates and tables of any kind the wrapper takes."""
+import pytest
+import torch
+
+from tests.test_train_gpu import _problem
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2607_22922_amd import ifvs
+    return ifvs
+
+
+def _scored(B, seed, cluster_cols=(0,), n_cand=300):
+    idx, ix, q, w_z, cand, preds, _ = _problem(B, seed, 16, 4, cluster_cols, nq=9, n_cand=n_cand)
+    alpha, wf = idx.select_codebook(q, preds, w_z)
+    return idx, ix, idx.build_lut(q, alpha, wf), cand
+
+
+def test_first_scores_on_two_streams(B):
+    """The first call on a clustered index makes the order's inverse; a call on
+    another stream right after it sees it whole."""
+    idx, ix, lut, cand = _scored(B, 41)
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(one):
+        torch.cuda._sleep(20_000_000)
+        a = idx.score_candidates(lut, cand)
+    with torch.cuda.stream(two):
+        b = idx.score_candidates(lut, cand)
+    torch.cuda.synchronize()
+    rows = ix["codes"].long()[cand.clamp(0, ix["codes"].shape[0] - 1).long()]
+    want = -torch.gather(lut.double(), 2, rows.permute(0, 2, 1)).sum(1)
+    there = (cand >= 0) & (cand < ix["codes"].shape[0])
+    assert torch.equal(a, b)
+    # 16 fp32 additions of table entries
+    assert torch.all((a.double() - want).abs()[there] <= 16 * 2.0 ** -24 * want.abs()[there])
+    assert torch.all(a[~there] == -float("inf"))
+
+
+def test_scores_in_a_captured_graph(B):
+    """The first call cannot be captured and says so; later ones can, and
+    replay with new tables."""
+    idx, _, lut, cand = _scored(B, 42)
+    torch.cuda.synchronize()
+    with pytest.raises(B.IfvsError) as e:
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            idx.score_candidates(lut, cand)
+    assert e.value.status == B.E_STATE
+    want = idx.score_candidates(lut, cand)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = idx.score_candidates(lut, cand)
+    for step in range(3):
+        lut.mul_(1.0 + step)
+        want = idx.score_candidates(lut, cand)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want), step
