@@ -20,6 +20,7 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libifvs.so
 OK, E_INVALID, E_NOMEM, E_HIP, E_UNSUPPORTED, E_STATE = 0, -1, -2, -3, -4, -5
 MEM_HOST, MEM_DEVICE = 0, 1
 LUT_F32, LUT_F16 = 0, 1
+LUT_TORCH = {LUT_F32: torch.float32, LUT_F16: torch.float16}
 KSUB = 256
 MAX_CLAUSES = 4
 MAX_K = 1024
@@ -444,6 +445,12 @@ class Index:
                              tau, lam, lr, loss, dwz)
         return loss, dwz
 
+    def _cand_arg(self, cand):
+        """Candidate ids as the calls take them: numbers past 32 bits are absent."""
+        if cand.dim() != 2:
+            raise IfvsError(E_INVALID, "cand must be [nq][n_cand]")
+        return _small_arg(cand, "cand", torch.int32, tuple(cand.shape), self.device)
+
     def score_candidates_into(self, nq, lut, lut_dtype, cand, logits_out, stream=None):
         """ifvs_score_candidates: -distance of each listed candidate."""
         _check(_lib.ifvs_score_candidates(self.handle, nq, lut.data_ptr(), lut_dtype, cand.data_ptr(), cand.shape[1],
@@ -451,10 +458,12 @@ class Index:
 
     def score_candidates(self, lut, cand, lut_dtype=LUT_F32):
         """[nq][n_cand] logits of the candidates (ids, -1 absent) under the
-        tables, for log_probs and distill_loss."""
-        cand = cand.to(dtype=torch.int32).contiguous()
-        if lut.shape[0] != cand.shape[0]:
-            raise IfvsError(E_INVALID, "lut and cand have different row counts")
+        tables (build_lut's, of type lut_dtype), for log_probs and distill_loss."""
+        cand = self._cand_arg(cand)
+        want = (cand.shape[0], self.m, KSUB)
+        if tuple(lut.shape) != want or lut.dtype != LUT_TORCH.get(lut_dtype) or lut.device != self.device:
+            raise IfvsError(E_INVALID, f"lut must be {want}, of the type lut_dtype names, on {self.device}")
+        lut = lut.contiguous()
         logits = torch.empty(cand.shape, device=self.device)
         self.score_candidates_into(cand.shape[0], lut, lut_dtype, cand, logits)
         return logits
@@ -470,17 +479,18 @@ class Index:
         """Marshalling wrapper: cand's first columns are the candidates whose
         teacher distances teacher_dist [nq][n_teacher] holds.  Returns
         (per-query loss, dL/dw_z or None)."""
-        q = q.contiguous()
-        cand = cand.to(dtype=torch.int32).contiguous()
+        nq = len(preds)
+        q = _small_arg(q, "q", torch.float32, (nq, self.dim), self.device)
+        w_z = _small_arg(w_z, "w_z", torch.float32, (nq, self.dim), self.device)
+        cand = self._cand_arg(cand)
+        if teacher_dist.dim() != 2:
+            raise IfvsError(E_INVALID, "teacher_dist must be [nq][n_teacher]")
         teacher_dist = _dev_f32(teacher_dist, self.device)
-        if cand.shape[0] != q.shape[0] or teacher_dist.shape[0] != q.shape[0]:
-            raise IfvsError(E_INVALID, "q, cand and teacher_dist have different row counts")
-        if w_z is not None and w_z.shape != q.shape:
-            raise IfvsError(E_INVALID, "w_z must have q's shape")
+        if cand.shape[0] != nq or teacher_dist.shape[0] != nq:
+            raise IfvsError(E_INVALID, "preds, cand and teacher_dist have different row counts")
         loss = torch.empty(q.shape[0], device=self.device)
         dwz = torch.empty_like(q) if want_dwz else None
-        self.distill_step_into(q, pack_predicates(preds), None if w_z is None else w_z.contiguous(), cand,
-                               teacher_dist, tau, lam, lr, loss, dwz)
+        self.distill_step_into(q, pack_predicates(preds), w_z, cand, teacher_dist, tau, lam, lr, loss, dwz)
         return loss, dwz
 
     def read_params(self):

@@ -61,3 +61,25 @@ def test_scores_in_a_captured_graph(B):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(got, want), step
+
+
+@pytest.mark.parametrize("cluster_cols", [(), (0,)])
+def test_candidates_and_tables_of_any_layout(B, cluster_cols):
+    """Wide ids (past 32 bits: absent), stepped ids and tables, and inputs of
+    the step in other float types give what 32-bit contiguous ones give."""
+    idx, ix, q, w_z, cand, preds, _ = _problem(B, 43, 16, 4, cluster_cols, nq=9, n_cand=40)
+    alpha, wf = idx.select_codebook(q, preds, w_z)
+    lut = idx.build_lut(q, alpha, wf)
+    want = idx.score_candidates(lut, cand)
+    assert torch.equal(idx.score_candidates(lut, cand.long()), want)
+    assert torch.equal(idx.score_candidates(lut, cand.repeat_interleave(2, 1)[:, ::2]), want)
+    assert torch.equal(idx.score_candidates(lut.repeat_interleave(2, 0)[::2], cand), want)
+    wide = cand.long() + (1 << 32)
+    assert torch.all(idx.score_candidates(lut, wide) == -float("inf"))
+    teacher = torch.rand(9, 4, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda") + 1
+    half = q.half()
+    ref = idx.distill_step(half.float(), preds, w_z, cand, teacher, 1.0, 0.1, 0.0, want_dwz=True)
+    got = idx.distill_step(half, preds, w_z, cand.long(), teacher.double(), 1.0, 0.1, 0.0, want_dwz=True)
+    torch.cuda.synchronize()
+    for a, b in zip(got, ref):
+        assert torch.equal(a, b)

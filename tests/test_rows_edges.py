@@ -78,3 +78,52 @@ def test_other_types_are_no_ids(bad):
     t = torch.zeros(3).to(bad)
     with pytest.raises(ifvs.IfvsError):
         ifvs._small_arg(t, "ids", torch.int32, (3,), t.device)
+
+
+def _bare_index():
+    """An index's Python side without a handle, on the CPU: a call that passes
+    the checks ends in the library with E_STATE."""
+    idx = ifvs.Index.__new__(ifvs.Index)
+    idx.handle, idx.device, idx.m, idx.dim = None, torch.device("cpu"), 4, 8
+    return idx
+
+
+LUT = torch.zeros(3, 4, 256)
+CAND = torch.zeros(3, 5, dtype=torch.int32)
+
+
+@pytest.mark.parametrize("lut,cand,dtype", [
+    (LUT.half(), CAND, ifvs.LUT_F32), (LUT, CAND, ifvs.LUT_F16), (LUT, CAND, 7), (LUT.double(), CAND, ifvs.LUT_F32),
+    (LUT[:2], CAND, ifvs.LUT_F32), (LUT[:, :3], CAND, ifvs.LUT_F32), (LUT[:, :, :255], CAND, ifvs.LUT_F32),
+    (LUT[0], CAND, ifvs.LUT_F32), (LUT.to("meta"), CAND, ifvs.LUT_F32), (LUT, CAND[0], ifvs.LUT_F32),
+    (LUT, CAND.float(), ifvs.LUT_F32), (LUT, CAND.to("meta"), ifvs.LUT_F32), (LUT, CAND[:2], ifvs.LUT_F32)],
+    ids=range(13))
+def test_candidate_scores_refuse_tables_they_would_read_past(lut, cand, dtype):
+    with pytest.raises(ifvs.IfvsError) as e:
+        _bare_index().score_candidates(lut, cand, dtype)
+    assert e.value.status == ifvs.E_INVALID
+
+
+Q = torch.zeros(3, 8)
+PREDS = [[(0, 0, 1)]] * 3
+STEP = dict(q=Q, preds=PREDS, w_z=Q, cand=CAND, teacher_dist=torch.ones(3, 2))
+
+
+@pytest.mark.parametrize("change", [
+    dict(q=Q[:, :7]), dict(q=Q[:2]), dict(q=Q[0]), dict(q=Q.to("meta")), dict(preds=PREDS[:2]), dict(w_z=Q[:, :7]),
+    dict(w_z=Q[:2]), dict(w_z=Q.to("meta")), dict(cand=CAND[:2]), dict(cand=CAND[0]), dict(cand=CAND.to("meta")),
+    dict(cand=CAND.double()), dict(teacher_dist=torch.ones(2, 2)), dict(teacher_dist=torch.ones(3))], ids=range(14))
+def test_distill_step_refuses_arrays_it_would_read_past(change):
+    with pytest.raises(ifvs.IfvsError) as e:
+        _bare_index().distill_step(**dict(STEP, **change), tau=1.0, lam=0.0, lr=0.0)
+    assert e.value.status == ifvs.E_INVALID
+
+
+def test_checked_calls_reach_the_library(monkeypatch):
+    monkeypatch.setattr(ifvs, "_stream", lambda stream: None)
+    for call in (lambda i: i.score_candidates(LUT, CAND), lambda i: i.score_candidates(LUT.half(), CAND, ifvs.LUT_F16),
+                 lambda i: i.distill_step(**STEP, tau=1.0, lam=0.0, lr=0.0),
+                 lambda i: i.distill_step(**dict(STEP, w_z=None, q=Q.half()), tau=1.0, lam=0.0, lr=0.0)):
+        with pytest.raises(ifvs.IfvsError) as e:
+            call(_bare_index())
+        assert e.value.status == ifvs.E_STATE
