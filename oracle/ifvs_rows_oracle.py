@@ -116,10 +116,12 @@ def distill(logits, teacher_ids, teacher_logits, tau=1.0, teacher_lse=None, row_
                 lq_rest = lq[~named]
                 lq_rest = lq_rest[~np.isneginf(lq_rest)]
                 if lq_rest.size:             # else no other column to give the rest to
-                    log_q_left = lq_rest.max() + np.log(np.exp(lq_rest - lq_rest.max()).sum())
+                    # shares from differences: far below the row's maximum a
+                    # logarithm no longer holds that of their sum
+                    e = np.exp(lq[~named] - lq_rest.max())
                     if left > 0:
-                        value += left * (np.log(left) - log_q_left)
-                    target[~named] = left * np.exp(lq[~named] - log_q_left)
+                        value += left * (np.log(left) - (lq_rest.max() + np.log(e.sum())))
+                    target[~named] = left * (e / e.sum())
         loss[i] = tau * tau * value
         grad[i, :m] = w * tau * (q - target)
     return loss, grad

@@ -127,3 +127,15 @@ def test_checked_calls_reach_the_library(monkeypatch):
         with pytest.raises(ifvs.IfvsError) as e:
             call(_bare_index())
         assert e.value.status == ifvs.E_STATE
+
+
+def test_definition_shares_the_rest_far_below_the_maximum():
+    """Others at one value far below the named column share the rest equally."""
+    for far in (-1e9, -1e13, -1e20, -3e38):
+        x = np.full((1, 101), far)
+        x[0, 7] = 0.0
+        loss, grad = R.distill(x, np.array([[7]]), np.array([[np.log(0.5)]]), teacher_lse=np.zeros(1))
+        want = np.full(101, -0.005)
+        want[7] = 0.5
+        assert np.allclose(grad[0], want, rtol=1e-12)
+        assert np.isclose(loss[0], 0.5 * np.log(0.5) + 0.5 * (np.log(0.5) - far - np.log(100)), rtol=1e-12)

@@ -2,11 +2,14 @@
 64-bit definitions: empty batches, logits far from 0, ties behind ragged ends,
 rows and teachers without a distribution, narrow ids.  Tolerances are those of
 test_rows_gpu.py."""
+import numpy as np
 import pytest
 import torch
 
+from oracle import ifvs_rows_oracle as R
 from tests._gpu_util import say
-from tests.test_rows_gpu import INF, TYPES, _check_distill, _check_log_probs, _gen, _row_view, _teacher
+from tests.test_rows_gpu import (HALF, INF, TINY, TYPES, U, _check_distill, _check_log_probs, _close, _gen, _np,
+                                 _row_view, _teacher)
 
 pytestmark = pytest.mark.gpu
 
@@ -107,6 +110,59 @@ def test_log_probs_far_from_zero(B, dtype, tau, cols):
     _check_log_probs(B, x, tau, None, given, 12)
 
 
+def _check_far_distill(B, x, ids, t, tau, lse, weight):
+    """The bounds of test_rows_gpu.py's check, but the other columns' shares of
+    the rest are taken from their logits' differences: far below the row's
+    maximum their q is 0 in 64 bits too, while the rest's gradient
+    -weight tau P q_v / Q is not.  With zo = (largest other - x) / tau a share
+    2^(x c - b) / S is off by u (3 zo + 6) (exponent and power), S by
+    u (3 E[zo] + 132), its product with the constant and the difference from
+    tau q by u each."""
+    loss, grad = B.distill_loss(x, ids, t, tau, lse, weight)
+    only, _ = B.distill_loss(x, ids, t, tau, lse, weight, want_grad=False)
+    mine = x.clone()
+    loss2, grad2 = B.distill_loss(mine, ids, t, tau, lse, weight)
+    loss3, grad3 = B.distill_loss(mine, ids, t, tau, lse, weight, grad_out=mine)
+    torch.cuda.synchronize()
+    bits = lambda a: a.contiguous().view(torch.int32 if a.dtype == torch.float32 else torch.int16)
+    assert torch.equal(bits(loss), bits(only)) and torch.equal(bits(loss2), bits(loss3))
+    assert torch.equal(bits(grad2), bits(grad3)), "the gradient in place differs"
+    x64, t64, at, wt = _np(x), _np(t), _np(ids), _np(weight)
+    tau = float(np.float32(tau))
+    w_loss, w_grad = R.distill(x64, at, t64, tau, None if lse is None else _np(lse), wt)
+    n, cols = x64.shape
+    loss_tol, grad_tol = np.zeros(n), np.zeros((n, cols))
+    for i in range(n):
+        lq = R.log_softmax(x64[i], tau)
+        if lq is None:
+            continue
+        z = (x64[i].max() - x64[i]) / tau
+        q = np.exp(lq)
+        lse_tol = U * (3 * (q[q > 0] * z[q > 0]).sum() + 132)
+        lp = R.log_softmax(t64[i], tau) if lse is None else t64[i] / tau - float(lse[i])
+        p = np.exp(lp)
+        target = np.zeros(cols)
+        np.add.at(target, at[i], p)
+        loss_tol[i] = (p * (lse_tol + 2 * U * np.where(np.isfinite(z[at[i]]), z[at[i]], 0))).sum()
+        rel = np.where(q > 0, lse_tol + U * (3 * np.where(q > 0, z, 0) + 6), 0)
+        tol = q * rel + U * (q + target)
+        others = np.isfinite(x64[i])
+        others[at[i]] = False
+        left = max(0.0, 1 - p.sum())
+        if lse is not None and others.any() and left > 0:
+            zo = z[others] - z[others].min()
+            qo = np.exp(-zo) / np.exp(-zo).sum()
+            rest_tol = U * (3 * (qo * zo).sum() + 132)
+            loss_tol[i] += left * (lse_tol + rest_tol + 4 * U * z[others].min())
+            tol[others] += left * qo * (rest_tol + U * (3 * zo + 8))
+        loss_tol[i] = tau * tau * loss_tol[i] + U * abs(np.nan_to_num(w_loss[i], posinf=0)) + 1e-12 * tau * tau
+        grad_tol[i] = wt[i] * tau * tol + (HALF[x.dtype] * (1 + 1e-3) + 2 * U) * np.abs(w_grad[i]) + TINY[x.dtype]
+    _close(_np(loss), w_loss, loss_tol, "loss")
+    _close(_np(loss2), w_loss, loss_tol, "the copy's loss")
+    _close(_np(grad), w_grad, grad_tol, "gradient")
+    _close(_np(grad2), w_grad, grad_tol, "the copy's gradient")
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rest", [False, True])
 @pytest.mark.parametrize("tau", [1.0, 1e-4, 1e-9])
@@ -125,7 +181,7 @@ def test_distill_far_from_zero(B, dtype, rest, tau, cols, n):
     if dtype != torch.float16:
         x[4, ids[4].long()] = torch.randn(6, generator=gen, device="cuda").to(dtype)
     weight = torch.rand(n, generator=gen, device="cuda") + 0.5
-    _check_distill(B, x, ids, t, tau, lse if rest else None, weight)
+    _check_far_distill(B, x, ids, t, tau, lse if rest else None, weight)
 
 
 @pytest.mark.parametrize("cols,n", [(50, 9), (3001, 9), (40001, 9), (40001, 131)])
