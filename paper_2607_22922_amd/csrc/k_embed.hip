@@ -138,14 +138,24 @@ constexpr int kSortTile = kSortThreads * kSortRounds;
 constexpr int kSortMaxBits = 10;
 constexpr int kSortMaxGroups = 256;
 // One launch (sort_owned_kernel) up to this many slots and owners: each owner
-// reads all ids, so its time grows with slots x owners, and the owner of a
-// frequent row sorts alone.  Gradients of 64 columns, uniform and skewed ids, us,
-// one launch against four: 8192 slots 21 and 31, 34 and 43; 16384 26 and 44, 37
-// and 48; 32768 40 and 75, 42 and 52; 131072 104 and 255, 51 and 88.  Twice as
-// many where a large table is cleared beside it anyway (21003 slots and 173 MB
-// 52 and 63, 32768 and 537 MB 142 and 148).
+// reads all ids, so its time grows with slots x owners, and the owner of
+// frequent rows sorts alone; the four launches of the radix sort cost the same
+// for any ids.  Whole gradients, one launch / four, us (45000 rows of 64
+// columns; ids uniform, Zipf scattered over the table, Zipf in its first rows,
+// half of them one row): 16384 slots 26/40, 36/44, 49/44, 60/61 (beyond, an
+// owner no longer holds the ids in registers); 20480 35/43, 42/45, 60/46,
+// 71/62; 32768 43/48, 57/50, 81/51, 93/71.
+// What is cleared beside the sort hides part of that: one slot more for every
+// 32 KB cleared, up to twice as many.  131072 rows, clearing 173 MiB (up to
+// 21920 slots): 20480 slots 51/65, 51/62, 79/62, 78/71, 24576 55/67, 58/62,
+// 90/63, 86/73; 256 MiB (24576): 20480 67/78, 65/72, 83/72, 79/82, 32768 74/85,
+// 76/78, 115/78, 112/91; 512 MiB (32768): 32768 139/146, 130/136, 149/132,
+// 142/147.  Over three heights of the table, eight sizes of the clear and 16384
+// to 32768 slots of those four kinds the choice costs 3.0% over the better of
+// the two in the mean and 35% at worst; 28 to 40 KB a slot do the same, a limit
+// of 16384 slots for all 4.0%, of 32768 from 128 MiB on 4.5% (79% at worst).
 constexpr int64_t kOwnedSlots = 1 << 14;
-constexpr int64_t kLongClear = 1 << 27;               // bytes
+constexpr int64_t kClearPerSlot = 1 << 15;            // bytes
 constexpr int kOwnersFull = 256;
 constexpr int64_t kMostOwners = 1 << 9;
 
@@ -693,7 +703,7 @@ EmbedPlan embed_plan(int64_t rows, int dim, int64_t slots, int64_t clear_bytes) 
   while ((rows >> bits) != 0) ++bits;                 // `rows` itself is a key
   int own = 6;
   while (own < kSortMaxBits && (rows >> own) >= kOwnersFull) ++own;
-  if (slots <= (clear_bytes >= kLongClear ? 2 : 1) * kOwnedSlots && (rows >> own) < kMostOwners) {
+  if (slots <= kOwnedSlots + std::min(clear_bytes / kClearPerSlot, kOwnedSlots) && (rows >> own) < kMostOwners) {
     p.bits = own;
     p.groups = static_cast<int>((rows >> own) + 1);
   } else {

@@ -248,3 +248,30 @@ def test_ids_of_any_whole_type(B, wide):
     if wide in (torch.int8, torch.int16, torch.int64):
         absent = torch.full((6, 1), -1, device="cuda", dtype=wide)
         assert torch.all(B.embed_lookup(x, absent) == 0) and torch.all(B.log_probs(x, absent)[0] == -INF)
+
+
+@pytest.mark.parametrize("kind", ["uniform", "skew"])
+@pytest.mark.parametrize("rows,dim", [(45000, 961), (8192, 2048), (300000, 33)])
+def test_gradients_around_the_longest_one_launch_sort(B, rows, dim, kind):
+    """One launch sorts as many slots as the clear beside it allows (one more
+    for every 32 KB beyond 16384), a radix sort the next: an absent slot more
+    changes nothing."""
+    limit = 16384 + min(rows * dim * 4 // 32768, 16384)
+    say(f"[longest one-launch sort] {rows} x {dim}, {limit} slots, {kind}")
+    gen = _gen(rows)
+    grad = torch.randn(limit + 1, dim, generator=gen, device="cuda")
+    ids = torch.randint(-1, rows, (limit + 1, 1), generator=gen, device="cuda", dtype=torch.int32)
+    if kind == "skew":
+        ids[torch.rand(limit + 1, 1, generator=gen, device="cuda") < 0.3] = rows // 3
+    ids[limit] = -1
+    one, two = B.embed_gradient(grad[:limit], ids[:limit], rows), B.embed_gradient(grad, ids, rows)
+    want = torch.zeros(rows + 1, dim, device="cuda", dtype=torch.float64)
+    size = torch.zeros_like(want)
+    flat = ids[:, 0].long() % (rows + 1)
+    want.index_add_(0, flat, grad.double())
+    size.index_add_(0, flat, grad.double().abs())
+    count = torch.bincount(flat, minlength=rows + 1)[:rows, None]
+    torch.cuda.synchronize()
+    assert torch.equal(one.view(torch.int32), two.view(torch.int32))
+    # as many fp32 additions as the row has slots, one rounding of the result
+    assert torch.all((one.double() - want[:rows]).abs() <= (count + 2) * U * size[:rows])
