@@ -162,8 +162,8 @@ def main(argv=None):
             entropy += float(h.sum())
             best += int(((top[:, 0] >= 0) & (top[:, 0] < k)).sum())
             n_rows += q.shape[0]
-        return {"logprob_of_neighbours": logp / max(n, 1), "entropy": entropy / n_rows,
-                "best_is_a_neighbour": best / n_rows}
+        return {"logprob_of_neighbours": logp / max(n, 1), "entropy": entropy / max(n_rows, 1),
+                "best_is_a_neighbour": best / max(n_rows, 1)}
 
     before = {"train": recall(train), "test": recall(test)}
     identity = {"train": recall(train, False), "test": recall(test, False)}

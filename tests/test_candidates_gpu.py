@@ -83,3 +83,12 @@ def test_candidates_and_tables_of_any_layout(B, cluster_cols):
     torch.cuda.synchronize()
     for a, b in zip(got, ref):
         assert torch.equal(a, b)
+
+
+def test_training_loop_without_training_queries(B):
+    """No training queries and no epochs: recall on the test queries alone."""
+    from paper_2607_22922_amd import train
+    out = train.main(["--config", "c1", "--bin", "0.1", "--train-queries", "0", "--test-queries", "32", "--batch",
+                      "32", "--epochs", "0", "--n-neg", "16"])
+    assert out["recall@10_conditioned_before"] == out["recall@10_identity"] == out["recall@10_conditioned_after"]
+    assert out["candidates_before"] == {"logprob_of_neighbours": 0.0, "entropy": 0.0, "best_is_a_neighbour": 0.0}
