@@ -469,7 +469,9 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(const LogProbArgs a,
 //
 // The loss is a difference of logarithms that may be 1e-3 of them, so the
 // exponents are computed with c in two parts (log2(e) / tau rounded to fp32
-// alone moves the temperature by 2^-25).  c_lo > 0, so that -inf stays -inf.
+// alone moves the temperature by 2^-25).  c_lo > 0, so that -inf stays -inf; from
+// tau = 1e37 on it may lie below the smallest fp32 number, which then stands for
+// it (and changes no exponent by more than 2^-21).
 struct SplitC {
   float hi, lo;
 };
@@ -477,7 +479,7 @@ struct SplitC {
 __device__ __forceinline__ SplitC split_c(double c) {
   float hi = static_cast<float>(c);
   if (hi >= c) hi = __uint_as_float(__float_as_uint(hi) - 1);
-  return {hi, static_cast<float>(c - hi)};
+  return {hi, fmaxf(static_cast<float>(c - hi), 0x1p-149f)};
 }
 
 // A chunk's sums: the others', relative to 2^other_origin, and the named

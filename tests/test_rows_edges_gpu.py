@@ -155,7 +155,9 @@ def _check_far_distill(B, x, ids, t, tau, lse, weight):
             rest_tol = U * (3 * (qo * zo).sum() + 132)
             loss_tol[i] += left * (lse_tol + rest_tol + 4 * U * z[others].min())
             tol[others] += left * qo * (rest_tol + U * (3 * zo + 8))
-        loss_tol[i] = tau * tau * loss_tol[i] + U * abs(np.nan_to_num(w_loss[i], posinf=0)) + 1e-12 * tau * tau
+        # below fp32's normal range (tau^2 may be 1e-75) rounding costs up to 2^-126, as for gradients
+        loss_tol[i] = tau * tau * loss_tol[i] + U * abs(np.nan_to_num(w_loss[i], posinf=0)) + 1e-12 * tau * tau \
+            + TINY[torch.float32]
         grad_tol[i] = wt[i] * tau * tol + (HALF[x.dtype] * (1 + 1e-3) + 2 * U) * np.abs(w_grad[i]) + TINY[x.dtype]
     _close(_np(loss), w_loss, loss_tol, "loss")
     _close(_np(loss2), w_loss, loss_tol, "the copy's loss")
@@ -275,3 +277,23 @@ def test_gradients_around_the_longest_one_launch_sort(B, rows, dim, kind):
     assert torch.equal(one.view(torch.int32), two.view(torch.int32))
     # as many fp32 additions as the row has slots, one rounding of the result
     assert torch.all((one.double() - want[:rows]).abs() <= (count + 2) * U * size[:rows])
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("tau", [3e-38, 2e30, 1e38, 1.3e38, 3e38])
+@pytest.mark.parametrize("cols,n", [(50, 20), (3001, 20), (40001, 20), (40001, 131)])
+def test_temperatures_at_the_ends_of_fp32(B, rest, tau, cols, n):
+    """Temperatures whose reciprocal is barely a number, with logits of that
+    size; masks of -inf.  (tau^2 times a divergence may pass fp32's range.)"""
+    say(f"[extreme tau] {tau} cols={cols} n={n} rest={rest}")
+    gen = _gen(cols)
+    x = _row_view(n, cols, torch.float32, gen, scale=min(tau, 5e37) if tau > 1 else 1e-37)
+    x[1, ::3] = -INF
+    x[2] = 0.0
+    x[3] = torch.finfo(torch.float32).min
+    ids = torch.rand(n, cols, generator=gen, device="cuda").topk(6, 1).indices.to(torch.int32)
+    t = torch.randn(n, 6, generator=gen, device="cuda") * (5e37 if tau > 1e37 else tau)
+    lse = torch.logsumexp(t / tau, 1) + 0.7
+    weight = torch.rand(n, generator=gen, device="cuda")
+    _check_log_probs(B, x, tau, None, ids, 12)
+    _check_far_distill(B, x, ids, t, tau, lse if rest else None, weight)
