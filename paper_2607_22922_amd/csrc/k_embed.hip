@@ -454,7 +454,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_move_kernel(const SortArgs 
 
 // ------------------------------------------------------------ summing runs
 // Sorted slots of a piece: about kPieces of them fill the GPU, up to kLongPiece
-// slots each; kMaxPieces bounds the longest join.
+// slots each; kMaxPieces bounds the longest join, so past 262144 slots a piece
+// has 1 / 8192 of them (of 2^30 slots 131072, added one after another).
 constexpr int64_t kPieces = 1024;
 constexpr int64_t kLongPiece = 32;
 constexpr int64_t kMaxPieces = 1 << 13;

@@ -385,7 +385,9 @@ __global__ __launch_bounds__(256) void train_update_bank_kernel(float* __restric
 
 // Scores of listed candidates (the Rank stage's distances, negated): a thread
 // per candidate, its table reads from the caches (a query's table is 16 to 120
-// KB and its candidates' workgroups read it together).
+// KB and its candidates' workgroups read it together).  Its chain of code words
+// and table entries bounds it: 256 queries x 42 candidates of M = 48 take 17 us
+// (fp16 tables 14; reading the tables once would take 2), x 4096 171 (156).
 constexpr int kScoreThreads = 256;
 template <typename L>
 __global__ __launch_bounds__(kScoreThreads) void score_candidates_kernel(const ScoreArgs a) {
